@@ -128,12 +128,13 @@ typedef struct {
 typedef enum {
   CFDETR_K_SELECT = 0, /* A2 cell tests, compaction, offsets                   */
   CFDETR_K_PLAN = 1,   /* attention work list from the sequence offsets; of the
-                          decoder also the tokens in bf16                      */
+                          decoder also the tokens in bf16; cell positions and
+                          the list of keys that a mask leaves                  */
   CFDETR_K_EMBED = 2,  /* patch gather + projection + position                 */
   CFDETR_K_GATHER = 3, /* reuse of cached coarse tokens                        */
-  CFDETR_K_LN = 4,     /* LayerNorm                                            */
-  CFDETR_K_QKV = 5,    /* query/key/value projection                           */
-  CFDETR_K_ATTN = 6,   /* variable-length self-attention                       */
+  CFDETR_K_LN = 4,     /* LayerNorm; norms with gate and residual              */
+  CFDETR_K_QKV = 5,    /* query/key/value projection, rotary positions         */
+  CFDETR_K_ATTN = 6,   /* variable-length self-attention, differential or not  */
   CFDETR_K_OUT = 7,    /* output projection + residual                         */
   CFDETR_K_FF1 = 8,    /* first FFN projection + GELU                          */
   CFDETR_K_FF2 = 9,    /* second FFN projection + residual; where one kernel does
@@ -425,6 +426,144 @@ CFDETR_API cfdetr_status cfdetr_decoder_attach(cfdetr_ctx* ctx, const cfdetr_dec
 CFDETR_API cfdetr_status cfdetr_decode(cfdetr_ctx* ctx, const float* memory,
                             const int32_t* cu_seqlens, int32_t B, float* queries,
                             void* hip_stream);
+
+/* ---- Differential encoder layers -------------------------------------------------------
+ *
+ * Three operators between the matrix products of an encoder layer, on the caller's rows, and a
+ * form of this library's encoder that is made of them.  They take their shape from the context:
+ * d = d_model columns, n_heads heads of d_head = d_model / n_heads, elements ("act") of act_dtype,
+ * eps = ln_eps.  Rows of act lie `ld` elements apart; a pointer to act rows, and ld times the element's
+ * size, are multiples of 16 bytes and ld >= d (else CFDETR_EINVAL).  Rows are never copied or
+ * moved; an output overlaps an input only where that is said.  The operators use the context's work
+ * space: the rule that calls on one context must not overlap holds for them as for the others.
+ */
+
+/*
+ * Rotary positions of the queries and keys of a head: pair i of n = rot_dim / 2 is turned by
+ * pos[axis] * f_i radians, (a, b) -> (a cos - b sin, a sin + b cos).
+ * With j = i mod (n / n_axes) the frequency is base^(-j n_axes / n); the first n / 2 pairs of two
+ * axes belong to axis 0.  For positions beyond the trained ones:
+ *   trained_len = 0   f_i = frequency / factor (positions squeezed)
+ *   trained_len > 0   by parts: a pair that turns keep_turns times or more over trained_len
+ *                     positions keeps its frequency, one that turns stretch_turns times or
+ *                     less has it divided by factor, those between a linear mixture of the two.
+ */
+typedef struct {
+  int32_t rot_dim;       /* features of a head that are rotated, from the first on: a multiple of
+                            16, at most d_head; the others stay as they are                   */
+  int32_t n_axes;        /* coordinates of a position: 1 or 2                                 */
+  int32_t interleaved;   /* 0: pair i = features i and i + n; 1: features 2i and 2i + 1       */
+  double base;           /* > 1, e.g. 10000                                                   */
+  double factor;         /* >= 1; 1: nothing is squeezed                                      */
+  double trained_len;    /* >= 0                                                              */
+  double keep_turns, stretch_turns;   /* keep_turns > stretch_turns >= 0 where trained_len > 0 */
+} cfdetr_rotary_params;
+
+/* Host only: freq [rot_dim / 2] (host) = f_i above.  All fields of `params` are checked (rot_dim
+ * at most 64); cfdetr_last_error(NULL) says why it failed. */
+CFDETR_API cfdetr_status cfdetr_rotary_frequencies(const cfdetr_rotary_params* params, double* freq);
+
+/*
+ * Rotated queries and keys of M rows (M = 0 does nothing).
+ *   params  host; rot_dim, n_axes and interleaved are used
+ *   freq    [rot_dim / 2] device, radians per unit of position (8-byte aligned), as
+ *           cfdetr_rotary_frequencies gives them or of the caller's own
+ *   pos     [M, n_axes] fp32 (4-byte aligned), exact for whole numbers up to 2^24; the angle is
+ *           worked out in 64 bits
+ *   q, k    [M, ld] act in: n_heads heads each; k and k_out may both be NULL
+ *   q_out, k_out  [M, ld] act out; q_out may be q and k_out may be k (with the same ld)
+ *   q_scale multiplies every feature of the queries before they are rounded: with
+ *           log2(e) / sqrt(d_head) the logits of cfdetr_diff_attention are base-2 already
+ */
+CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_params* params,
+                            const double* freq, const float* pos, int32_t M, const void* q,
+                            int32_t q_ld, void* q_out, int32_t q_out_ld, float q_scale,
+                            const void* k, int32_t k_ld, void* k_out, int32_t k_out_ld,
+                            void* hip_stream);
+
+/*
+ * Differential attention of the query rows of B frames over the token rows of the same frames
+ * (self-attention: the same offsets for both).  n_heads must be even (else CFDETR_ESHAPE): head h
+ * of n_heads / 2 has the query and key heads 2h and 2h + 1 and the values of width 2 d_head
+ * that lie in the columns of both.  With A_1 and A_2 the softmax over the frame's keys of
+ * softmax_scale q k^T of the two, a row is (A_1 - lambda[h] A_2) v, and with head_g
+ * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.
+ *   q [n_q, ld], k and v [n_k, ld] act; n_q, n_k <= max_tokens_total (else CFDETR_ECAPACITY)
+ *   cu_q, cu_k  [B+1] int32 device: offsets of the frames' rows, from 0; frames may be empty.
+ *               Negative lengths, or an end beyond n_q or n_k, make the call write nothing, and
+ *               cfdetr_sync_status reports CFDETR_ECAPACITY.
+ *   key_mask    [n_k] uint8 device, 0: no query reads that token, whatever it holds; NULL: all are read
+ *   lambda      [n_heads / 2] fp32 device
+ *   head_g      [2 d_head] fp32 device (16-byte aligned), shared by the heads; NULL: no norm
+ *   softmax_scale  > 0; or 0: the queries have been multiplied by log2(e) / sqrt(d_head) already
+ *   out [n_q, ld] act: head h in columns 2 h d_head on; may be q (with the same ld).  A row whose
+ *               frame has no key that may be read is 0.  Rows past cu_q[B] are untouched.
+ * Sums over many keys may be split over the chip; they are added in a fixed order, so the same
+ * call gives the same bits.
+ */
+CFDETR_API cfdetr_status cfdetr_diff_attention(cfdetr_ctx* ctx, const void* q, int32_t q_ld, int32_t n_q,
+                                    const void* k, int32_t k_ld, const void* v, int32_t v_ld,
+                                    int32_t n_k, const int32_t* cu_q, const int32_t* cu_k,
+                                    int32_t B, const uint8_t* key_mask, const float* lambda,
+                                    const float* head_g, float softmax_scale, void* out,
+                                    int32_t out_ld, void* hip_stream);
+
+typedef enum {
+  CFDETR_NORM_NONE = 0,
+  CFDETR_NORM_LAYER = 1, /* (v - mean) / sqrt(variance + eps) * gain + offset */
+  CFDETR_NORM_RMS = 2    /* v / sqrt(mean of squares + eps) * gain            */
+} cfdetr_norm;
+
+/* Parameters of cfdetr_norm_residual (host structure; vectors on the device, 16-byte aligned). */
+typedef struct {
+  cfdetr_norm post, pre;        /* norm behind the block and norm in front of the next            */
+  const float *post_g, *post_b; /* [d]; gain of a norm that is not NONE; offset of LAYER or NULL  */
+  const float *pre_g, *pre_b;
+  const float* gate;            /* NULL: 1; [d], or with cu_seqlens [B, d]: one for every frame   */
+  const int32_t* cu_seqlens;    /* NULL, or [B+1] int32 device: offsets of the frames, from 0      */
+  int32_t B;                    /* frames of cu_seqlens                                            */
+  float res_scale;              /* e.g. 1                                                          */
+} cfdetr_norm_residual_params;
+
+/*
+ * The step between two blocks, for M rows (M = 0 does nothing), in one pass:
+ *   x_out = res_scale * x + gate * post(block);   normed = pre(x_out)
+ *   x, x_out [M, d] fp32, 16-byte aligned; x_out may be x
+ *   block    [M, d] act, 16-byte aligned
+ *   normed   [M, d] act out, 16-byte aligned; may be block; NULL if and only if pre is NONE
+ * With cu_seqlens, rows past cu_seqlens[B] are untouched; a negative length or an end beyond M makes
+ * the call write nothing, and cfdetr_sync_status reports CFDETR_ECAPACITY.
+ */
+CFDETR_API cfdetr_status cfdetr_norm_residual(cfdetr_ctx* ctx, const cfdetr_norm_residual_params* params,
+                                   const float* x, const void* block, float* x_out, void* normed,
+                                   int32_t M, void* hip_stream);
+
+/*
+ * Weights of the differential form of the encoder's layers, beside those of cfdetr_create
+ * (device pointers, fp32, 16-byte aligned; stacked over the layers).
+ */
+typedef struct {
+  const float* lambda;            /* [L, n_heads / 2]                                              */
+  const float* head_g;            /* [L, 2 d_head], or NULL: no norm of the heads                  */
+  const float *post1_g, *post2_g; /* [L, d] gains of RMS norms behind attention and feed-forward,
+                                     or both NULL: no such norms                                  */
+  const float *gate1, *gate2;     /* [L, d] gates of the two blocks, or both NULL                  */
+  float res_scale;                /* of both residuals                                             */
+  cfdetr_rotary_params rotary;    /* n_axes = 2                                                    */
+} cfdetr_differential_weights;
+
+/*
+ * From here on the encode calls of this context (coarse, fine, padded, multilevel batch) run
+ * layers of the differential form, with the matrices, biases and LayerNorms of cfdetr_create:
+ *   q, k, v = Wqkv LN1 x;  q, k turned by the position of the token's cell
+ *   x <- res_scale x + gate1 * post1(Wo differential attention(q, k, v))
+ *   x <- res_scale x + gate2 * post2(W2 GELU(W1 LN2 x))
+ * and LNf behind the last.  A token's position is the (row, column) of its cell's centre in cells
+ * of the finest level, whatever its level; the position of the embedding stays.  n_heads must
+ * be even (else CFDETR_ESHAPE).  The structure is copied, the weights must outlive the context, some
+ * more work space is allocated.  A context is attached to once.  cfdetr_decode is as before.
+ */
+CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdetr_differential_weights* w);
 
 /* ------------------------------------------------------------------------
  * NPFP** scheduling decisions (Sec. IV).  Host memory only; no GPU work, no context,

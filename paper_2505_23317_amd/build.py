@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcfdetr.so")
 SOURCES = ["api.hip", "select.hip", "roi.hip", "rowwise.hip", "gemm.hip", "layer.hip", "small_layer.hip",
-           "few_rows.hip", "attention.hip", "sched.hip"]
+           "few_rows.hip", "attention.hip", "sched.hip", "rotary.hip", "diff_attention.hip", "norm_residual.hip"]
 # A kernel's first 14 words of arguments come in scalar registers with the launch, so that its first
 # loads need not wait for a load of their addresses (arguments that are structs are left in memory).
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hidden",

@@ -36,6 +36,8 @@ EXPORTS = [
     "cfdetr_multilevel_batch", "cfdetr_profile_begin", "cfdetr_profile_end",
     "cfdetr_sched_response_times", "cfdetr_sched_coarse_batch", "cfdetr_sched_fine_batches",
     "cfdetr_sched_decide", "cfdetr_decoder_attach", "cfdetr_decode", "cfdetr_merge_detections",
+    "cfdetr_rotary_frequencies", "cfdetr_rotary", "cfdetr_diff_attention", "cfdetr_norm_residual",
+    "cfdetr_differential_attach",
 ]
 POLICIES = {"C": 0, "CF": 1, "[C]F": 2, "C[F]": 3, "[C][F]": 4}
 SCHED_ACTIONS = ["idle", "coarse", "fine"]
@@ -85,6 +87,31 @@ DECODER_FIELDS = ("query_embed", "ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o
 class CfdetrDecoderWeights(ctypes.Structure):
     _fields_ = ([("n_queries", ctypes.c_int32), ("n_layers", ctypes.c_int32)]
                 + [(name, ctypes.c_void_p) for name in DECODER_FIELDS])
+
+
+NORMS = {"none": 0, "layer": 1, "rms": 2}
+
+
+class CfdetrRotaryParams(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("trained_len", ctypes.c_double),
+                ("keep_turns", ctypes.c_double), ("stretch_turns", ctypes.c_double)]
+
+
+class CfdetrNormResidualParams(ctypes.Structure):
+    _fields_ = [("post", ctypes.c_int), ("pre", ctypes.c_int),
+                ("post_g", ctypes.c_void_p), ("post_b", ctypes.c_void_p),
+                ("pre_g", ctypes.c_void_p), ("pre_b", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("res_scale", ctypes.c_float)]
+
+
+DIFFERENTIAL_FIELDS = ("lambda", "head_g", "post1_g", "post2_g", "gate1", "gate2")
+
+
+class CfdetrDifferentialWeights(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_void_p) for name in DIFFERENTIAL_FIELDS]
+                + [("res_scale", ctypes.c_float), ("rotary", CfdetrRotaryParams)])
 
 
 _lib = None
@@ -148,6 +175,18 @@ def load_library() -> ctypes.CDLL:
     lib.cfdetr_decoder_attach.restype = ctypes.c_int
     lib.cfdetr_decode.argtypes = [vp, vp, vp, i32, vp, vp]
     lib.cfdetr_decode.restype = ctypes.c_int
+    rot, f32 = ctypes.POINTER(CfdetrRotaryParams), ctypes.c_float
+    lib.cfdetr_rotary_frequencies.argtypes = [rot, dp]
+    lib.cfdetr_rotary_frequencies.restype = ctypes.c_int
+    lib.cfdetr_rotary.argtypes = [vp, rot, vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, vp, i32, vp]
+    lib.cfdetr_rotary.restype = ctypes.c_int
+    lib.cfdetr_diff_attention.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, i32, vp, vp, i32, vp, vp, vp,
+                                          f32, vp, i32, vp]
+    lib.cfdetr_diff_attention.restype = ctypes.c_int
+    lib.cfdetr_norm_residual.argtypes = [vp, ctypes.POINTER(CfdetrNormResidualParams), vp, vp, vp, vp, i32, vp]
+    lib.cfdetr_norm_residual.restype = ctypes.c_int
+    lib.cfdetr_differential_attach.argtypes = [vp, ctypes.POINTER(CfdetrDifferentialWeights)]
+    lib.cfdetr_differential_attach.restype = ctypes.c_int
     lib.cfdetr_profile_begin.argtypes = [vp]
     lib.cfdetr_profile_begin.restype = ctypes.c_int
     lib.cfdetr_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_float),
@@ -329,6 +368,58 @@ def cfdetr_sched_decide(policy: str, t, active_coarse, active_fine, fine_workloa
     return name, []
 
 
+def rotary_params(rot_dim: int, n_axes: int = 2, interleaved: bool = False, base: float = 10000.0,
+                  factor: float = 1.0, trained_len: float = 0.0, keep_turns: float = 32.0,
+                  stretch_turns: float = 1.0) -> CfdetrRotaryParams:
+    return CfdetrRotaryParams(rot_dim, n_axes, int(interleaved), base, factor, trained_len, keep_turns,
+                              stretch_turns)
+
+
+def cfdetr_rotary_frequencies(params: CfdetrRotaryParams):
+    """The rot_dim / 2 frequencies as a list (host)."""
+    # (a bad rot_dim is refused before anything is written)
+    freq = (ctypes.c_double * max(1, params.rot_dim // 2))()
+    _check(load_library().cfdetr_rotary_frequencies(ctypes.byref(params), freq))
+    return list(freq)
+
+
+def cfdetr_rotary(ctx, params: CfdetrRotaryParams, freq, pos, M, q, q_ld, q_out, q_out_ld, q_scale, k, k_ld,
+                  k_out, k_out_ld, stream=0) -> None:
+    _check(load_library().cfdetr_rotary(ctx, ctypes.byref(params), freq, pos, M, q, q_ld, q_out, q_out_ld,
+                                        q_scale, k, k_ld, k_out, k_out_ld, stream), ctx)
+
+
+def cfdetr_diff_attention(ctx, q, q_ld, n_q, k, k_ld, v, v_ld, n_k, cu_q, cu_k, B, key_mask, lambda_, head_g,
+                          softmax_scale, out, out_ld, stream=0) -> None:
+    _check(load_library().cfdetr_diff_attention(ctx, q, q_ld, n_q, k, k_ld, v, v_ld, n_k, cu_q, cu_k, B,
+                                                key_mask, lambda_, head_g, softmax_scale, out, out_ld,
+                                                stream), ctx)
+
+
+def norm_residual_params(post="none", pre="none", post_g=None, post_b=None, pre_g=None, pre_b=None, gate=None,
+                         cu_seqlens=None, res_scale=1.0) -> CfdetrNormResidualParams:
+    """post, pre: "none", "layer" or "rms"; the vectors are float32 device tensors (cu_seqlens int32), which
+    the structure keeps alive."""
+    p = CfdetrNormResidualParams(NORMS[post], NORMS[pre])
+    p.tensors = dict(post_g=post_g, post_b=post_b, pre_g=pre_g, pre_b=pre_b, gate=gate, cu_seqlens=cu_seqlens)
+    for name, t in p.tensors.items():
+        if t is not None:
+            _expect(t, "int32" if name == "cu_seqlens" else "float32", name)
+            setattr(p, name, t.data_ptr())
+    p.B = int(cu_seqlens.shape[0]) - 1 if cu_seqlens is not None else 0
+    p.res_scale = res_scale
+    return p
+
+
+def cfdetr_norm_residual(ctx, params: CfdetrNormResidualParams, x, block, x_out, normed, M, stream=0) -> None:
+    _check(load_library().cfdetr_norm_residual(ctx, ctypes.byref(params), x, block, x_out, normed, M, stream),
+           ctx)
+
+
+def cfdetr_differential_attach(ctx, weights: CfdetrDifferentialWeights) -> None:
+    _check(load_library().cfdetr_differential_attach(ctx, ctypes.byref(weights)), ctx)
+
+
 def cfdetr_profile_begin(ctx) -> None:
     _check(load_library().cfdetr_profile_begin(ctx), ctx)
 
@@ -350,6 +441,19 @@ def _to_device(arr: np.ndarray, as_bf16: bool):
         bits = synth.bf16_bits(arr).view(np.int16)
         return torch.from_numpy(bits).view(torch.bfloat16).reshape(arr.shape).cuda()
     return torch.from_numpy(np.ascontiguousarray(arr, dtype=np.float32)).cuda()
+
+
+def _expect(t, dtype: str, what: str, shape=None) -> None:
+    """A tensor that the library takes as it lies: contiguous, on the GPU, of the named type and shape."""
+    import torch
+    if t.dtype != getattr(torch, dtype) or not t.is_cuda or not t.is_contiguous() or (
+            shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: contiguous {dtype} on the GPU expected"
+                         + (f", shape {tuple(shape)}" if shape is not None else ""))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def unpack_tok_desc(desc: np.ndarray) -> np.ndarray:
@@ -396,6 +500,7 @@ class Encoder:
                      "w_ff1", "b_ff1", "w_ff2", "b_ff2", "lnf_g", "lnf_b"):
             setattr(w, name, self.dev[name].data_ptr())
         self.c_cfg, self.c_w = c, w
+        self.act = torch.bfloat16 if self.act_bf16 else torch.float32
         self.ctx = cfdetr_create(c, w)
 
     # -- helpers ---------------------------------------------------------------
@@ -518,6 +623,71 @@ class Encoder:
                                 out["y_mixed"].data_ptr(), out["tok_desc"].data_ptr(),
                                 out["cu_seqlens"].data_ptr(), out["level_counts"].data_ptr(),
                                 self._stream())
+
+    # -- operators of a differential layer, on the caller's rows -------------------------
+    def _rows(self, t, rows: int, what: str) -> int:
+        """Elements from row to row of a [rows, d] tensor in act_dtype whose rows are contiguous."""
+        if t.dtype != self.act or not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or (
+                t.shape[1] != self.cfg.d or t.stride(1) != 1):
+            raise ValueError(f"{what}: [{rows}, {self.cfg.d}] rows of {self.act} on the GPU expected")
+        return t.stride(0) if rows > 1 else self.cfg.d
+
+    def rotary(self, params: CfdetrRotaryParams, freq, pos, q, q_out, k=None, k_out=None, q_scale=1.0):
+        """freq: float64 [rot_dim / 2], pos: float32 [M, n_axes]; q, k and the outputs: [M, d] in act_dtype,
+        rows may lie apart (columns of a wider tensor)."""
+        M = int(q.shape[0])
+        _expect(freq, "float64", "freq", (params.rot_dim // 2,))
+        _expect(pos, "float32", "pos", (M, params.n_axes))
+        if (k is None) != (k_out is None):
+            raise ValueError("k and k_out go together")
+        q_ld, qo_ld = self._rows(q, M, "q"), self._rows(q_out, M, "q_out")
+        k_ld, ko_ld = (self._rows(k, M, "k"), self._rows(k_out, M, "k_out")) if k is not None else (0, 0)
+        cfdetr_rotary(self.ctx, params, freq.data_ptr(), pos.data_ptr(), M, q.data_ptr(), q_ld, q_out.data_ptr(),
+                      qo_ld, q_scale, _ptr(k), k_ld, _ptr(k_out), ko_ld, self._stream())
+
+    def diff_attention(self, q, k, v, cu_q, cu_k, lambda_, out, head_g=None, key_mask=None, softmax_scale=None):
+        """q, out: [n_q, d]; k, v: [n_k, d]; cu_q, cu_k: int32 [B + 1]; lambda_: float32 [n_heads / 2]; head_g:
+        float32 [2 d_head] or None; key_mask: uint8 [n_k] or None.  softmax_scale: None for 1 / sqrt(d_head), 0 for
+        queries that have been multiplied by log2(e) / sqrt(d_head)."""
+        n_q, n_k, B = int(q.shape[0]), int(k.shape[0]), int(cu_q.shape[0]) - 1
+        _expect(cu_q, "int32", "cu_q", (B + 1,))
+        _expect(cu_k, "int32", "cu_k", (B + 1,))
+        _expect(lambda_, "float32", "lambda_", (self.cfg.heads // 2,))
+        if head_g is not None:
+            _expect(head_g, "float32", "head_g", (2 * self.cfg.d_head,))
+        if key_mask is not None:
+            _expect(key_mask, "uint8", "key_mask", (n_k,))
+        if softmax_scale is None:
+            softmax_scale = self.cfg.d_head ** -0.5
+        cfdetr_diff_attention(self.ctx, q.data_ptr(), self._rows(q, n_q, "q"), n_q, k.data_ptr(),
+                              self._rows(k, n_k, "k"), v.data_ptr(), self._rows(v, n_k, "v"), n_k, cu_q.data_ptr(),
+                              cu_k.data_ptr(), B, _ptr(key_mask), lambda_.data_ptr(), _ptr(head_g), softmax_scale,
+                              out.data_ptr(), self._rows(out, n_q, "out"), self._stream())
+
+    def norm_residual(self, params: CfdetrNormResidualParams, x, block, x_out, normed=None):
+        """x, x_out: float32 [M, d]; block, normed: [M, d] in act_dtype, contiguous."""
+        M, d, act = int(x.shape[0]), self.cfg.d, "bfloat16" if self.act_bf16 else "float32"
+        for name, t in params.tensors.items():
+            if t is not None and name != "cu_seqlens" and t.numel() != (params.B * d if name == "gate" and params.B else d):
+                raise ValueError(f"{name}: {d} columns expected, and a row for every frame of cu_seqlens in the gate")
+        _expect(x, "float32", "x", (M, d))
+        _expect(block, act, "block", (M, d))
+        _expect(x_out, "float32", "x_out", (M, d))
+        if normed is not None:
+            _expect(normed, act, "normed", (M, d))
+        cfdetr_norm_residual(self.ctx, params, x.data_ptr(), block.data_ptr(), x_out.data_ptr(), _ptr(normed), M,
+                             self._stream())
+
+    def attach_differential(self, weights: Dict[str, np.ndarray], rotary: CfdetrRotaryParams, res_scale: float = 1.0):
+        """weights: float32 numpy arrays named as include/cfdetr.h lists them ("lambda", and any of "head_g",
+        "post1_g", "post2_g", "gate1", "gate2"); uploaded here and kept alive with the context."""
+        dev = {k: _to_device(v, False) for k, v in weights.items()}
+        w = CfdetrDifferentialWeights()
+        for name, t in dev.items():
+            setattr(w, name, t.data_ptr())
+        w.res_scale, w.rotary = res_scale, rotary
+        cfdetr_differential_attach(self.ctx, w)
+        self.diff_dev, self.c_diff = dev, w
 
     def sync_status(self):
         cfdetr_sync_status(self.ctx, self._stream())

@@ -3,6 +3,7 @@
 #include "../../include/cfdetr.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -105,6 +106,13 @@ struct cfdetr_ctx {
        *dslim_ff2 = nullptr, *dslim_box1 = nullptr, *dslim_box2 = nullptr;
   float* dz = nullptr;            // final LayerNorm of the queries in fp32 (fused path)
 
+  // layers of the differential form (cfdetr_differential_attach): their own allocation
+  bool has_diff = false;
+  cfdetr_differential_weights fw;
+  void* diff_arena = nullptr;
+  double* diff_freq = nullptr;    // [rot_dim / 2]
+  float* diff_pos = nullptr;      // [Tm, 2] positions of the rows of the run in flight
+
   std::string err;
 
   bool prof = false;
@@ -205,6 +213,43 @@ const char* check_config(const cfdetr_config& c) {
   return nullptr;
 }
 
+// Fields of a rotation that the kernel uses, for heads of `d_head`; with `table` also those of its frequencies.
+const char* check_rotary(const cfdetr_rotary_params& p, int d_head, bool table) {
+  if (p.rot_dim < 16 || p.rot_dim % 16 || p.rot_dim > d_head) return "rot_dim must be a multiple of 16, at most the head width";
+  if (p.n_axes != 1 && p.n_axes != 2) return "n_axes must be 1 or 2";
+  if (p.interleaved != 0 && p.interleaved != 1) return "interleaved must be 0 or 1";
+  if (!table) return nullptr;
+  if (!(p.base > 1.0) || !std::isfinite(p.base)) return "base must be a number above 1";
+  if (!(p.factor >= 1.0) || !std::isfinite(p.factor)) return "factor must be a number, at least 1";
+  if (!(p.trained_len >= 0.0) || !std::isfinite(p.trained_len)) return "trained_len must be a number, at least 0";
+  if (p.trained_len > 0.0 && !(p.stretch_turns >= 0.0 && p.keep_turns > p.stretch_turns && std::isfinite(p.keep_turns)))
+    return "keep_turns must be above stretch_turns, and that at least 0";
+  return nullptr;
+}
+
+void rotary_frequencies(const cfdetr_rotary_params& p, double* freq) {
+  const int n = p.rot_dim / 2, per_axis = n / p.n_axes;
+  for (int i = 0; i < n; ++i) {
+    double f = std::pow(p.base, -(double)(i % per_axis) / per_axis);
+    if (p.trained_len > 0.0) {
+      const double turns = p.trained_len * f / 6.283185307179586477;
+      const double keep = std::min(1.0, std::max(0.0, (turns - p.stretch_turns) / (p.keep_turns - p.stretch_turns)));
+      f *= keep + (1.0 - keep) / p.factor;
+    } else {
+      f /= p.factor;
+    }
+    freq[i] = f;
+  }
+}
+
+// Rows of act elements that an operator reads or writes.
+const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld) {
+  if (!p) return "null pointer";
+  if (ld < ctx->cfg.d_model) return "rows are shorter than d_model";
+  if (!aligned16(p) || (size_t)ld * ctx->esz % 16) return "rows must begin on multiples of 16 bytes";
+  return nullptr;
+}
+
 struct Carver {
   uint64_t off = 0;
   uint64_t take(uint64_t bytes) {
@@ -234,15 +279,20 @@ void prof_close(cfdetr_ctx* c, hipStream_t s) {
     if (e__ != hipSuccess) return fail_hip(ctx, #expr, e__);        \
   } while (0)
 
-cfdetr_status check_call(cfdetr_ctx* ctx, int B) {
+cfdetr_status check_device(cfdetr_ctx* ctx) {
   if (!ctx) return CFDETR_EINVAL;
-  if (B < 1) return fail(ctx, CFDETR_EINVAL, "B must be >= 1");
-  if (B > ctx->cfg.max_batch) return fail(ctx, CFDETR_ECAPACITY, "B exceeds max_batch");
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return fail_hip(ctx, "hipGetDevice", e);
   if (dev != ctx->device) return fail(ctx, CFDETR_EINVAL, "context belongs to another device");
   return CFDETR_OK;
+}
+
+cfdetr_status check_call(cfdetr_ctx* ctx, int B) {
+  if (!ctx) return CFDETR_EINVAL;
+  if (B < 1) return fail(ctx, CFDETR_EINVAL, "B must be >= 1");
+  if (B > ctx->cfg.max_batch) return fail(ctx, CFDETR_ECAPACITY, "B exceeds max_batch");
+  return check_device(ctx);
 }
 
 // Patch embedding of the tokens of one level into ctx->x (and optionally out2).
@@ -347,14 +397,118 @@ void ask_for(ReadAhead& ahead, int i, const void* at, size_t bytes) {
   ahead.bytes[i] = (uint32_t)bytes;
 }
 
+// Which cells the rows of a run are: descriptors of the first n_first rows, and of those behind.
+struct RunCells {
+  const int32_t* first;
+  int n_first;
+  const int32_t* second;
+};
+
+// Work space that an attention may have for partial results: the feed-forward block's hidden rows.
+uint64_t partial_bytes(const cfdetr_ctx* ctx) { return (ctx->tok_cap + 31) * (uint64_t)ctx->cfg.d_ffn * ctx->esz; }
+
+// All layers of the differential form and the final LayerNorm, as run_encoder does it.
+cfdetr_status run_differential(cfdetr_ctx* ctx, int nseq, const RunShape& shape, int m_cap, const RunCells& cells, float* y0,
+                               int split_row, float* y1, hipStream_t s, const int32_t* kv_len, bool rows_known) {
+  const cfdetr_config& c = ctx->cfg;
+  const cfdetr_weights& w = ctx->w;
+  const cfdetr_differential_weights& f = ctx->fw;
+  const size_t d = c.d_model, F = c.d_ffn, es = ctx->esz;
+  const int dh = c.d_model / c.n_heads;
+  const bool bf = ctx->bf16;
+  const int32_t* m_ptr = rows_known ? nullptr : ctx->m_all;
+  const int m_hint = rows_known ? m_cap : shape.rows;
+  auto mat = [&](const void* base, size_t elements) { return static_cast<const char*>(base) + elements * es; };
+
+  RotaryArgs ra{};
+  ra.q = ra.q_out = ctx->qkv;
+  ra.k = ra.k_out = static_cast<char*>(ctx->qkv) + d * es;
+  ra.q_ld = ra.k_ld = ra.qo_ld = ra.ko_ld = 3 * (int)d;
+  ra.pos = ctx->diff_pos;
+  ra.freq = ctx->diff_freq;
+  ra.m_ptr = m_ptr;
+  ra.m_capacity = m_cap;
+  ra.heads = c.n_heads;
+  ra.d_head = dh;
+  ra.rot_dim = f.rotary.rot_dim;
+  ra.n_axes = f.rotary.n_axes;
+  ra.interleaved = f.rotary.interleaved != 0;
+  ra.q_scale = attention_q_scale(dh);
+
+  DiffAttentionArgs aa{};
+  aa.q = ctx->qkv;
+  aa.k = ra.k;
+  aa.v = static_cast<char*>(ctx->qkv) + 2 * d * es;
+  aa.q_ld = aa.k_ld = aa.v_ld = 3 * (int)d;
+  aa.out = ctx->o;
+  aa.out_ld = (int)d;
+  aa.n_q = aa.n_k = m_cap;
+  aa.cu_q = aa.cu_k = ctx->cu_all;
+  aa.B = nseq;
+  aa.kv_len = kv_len;
+  aa.scale2 = 1.0f;   // in the rotation
+  aa.eps = c.ln_eps;
+  aa.heads = c.n_heads / 2;
+  const int rows = m_hint > 0 ? m_hint : m_cap;
+  aa.splits = diff_attention_splits(rows, rows, nseq, aa.heads, dh, partial_bytes(ctx) / m_cap * rows, ctx->cus);
+  aa.partial = static_cast<float*>(ctx->h);
+  aa.err_flag = ctx->err_flag;
+
+  NormResidualArgs na{};
+  na.block = ctx->a;
+  na.x = na.x_out = ctx->x;
+  na.post = f.post1_g ? NormKind::kRms : NormKind::kNone;
+  na.pre = NormKind::kLayer;
+  na.res_scale = f.res_scale;
+  na.eps = c.ln_eps;
+  na.d = (int)d;
+  na.m_ptr = m_ptr;
+  na.err_flag = ctx->err_flag;
+
+  CF_LAUNCH(CFDETR_K_PLAN, launch_cell_positions(cells.first, cells.n_first, cells.second, c.n_levels - 1, m_ptr, m_cap, ctx->diff_pos, s));
+  CF_LAUNCH(CFDETR_K_LN, launch_layernorm(ctx->x, w.ln1_g, w.ln1_b, ctx->a, bf, (int)d, c.ln_eps, m_ptr, m_cap, m_cap, 0, nullptr, s));
+  for (size_t l = 0; l < (size_t)c.n_layers; ++l) {
+    const bool last = l + 1 == (size_t)c.n_layers;
+    CF_LAUNCH(CFDETR_K_QKV, launch_gemm(ctx->a, mat(w.w_qkv, l * 3 * d * d), w.b_qkv + l * 3 * d, 3 * (int)d, (int)d, Epilogue::kBias,
+                                        ctx->qkv, nullptr, bf, m_ptr, m_hint, m_cap, s, 1.0f, packed(ctx->slim_qkv, l * 3 * d * d)));
+    CF_LAUNCH(CFDETR_K_QKV, launch_rotary(ra, bf, s));
+    aa.lambda = f.lambda + l * aa.heads;
+    aa.head_g = f.head_g ? f.head_g + l * 2 * dh : nullptr;
+    CF_LAUNCH(CFDETR_K_ATTN, launch_diff_attention(aa, dh, bf, s));
+    CF_LAUNCH(CFDETR_K_OUT, launch_gemm(ctx->o, mat(w.w_o, l * d * d), w.b_o + l * d, (int)d, (int)d, Epilogue::kBias, ctx->a, nullptr, bf,
+                                        m_ptr, m_hint, m_cap, s, 1.0f, packed(ctx->slim_o, l * d * d)));
+    na.post_g = f.post1_g ? f.post1_g + l * d : nullptr;
+    na.gate = f.gate1 ? f.gate1 + l * d : nullptr;
+    na.pre_g = w.ln2_g + l * d;
+    na.pre_b = w.ln2_b + l * d;
+    na.normed = ctx->o;
+    CF_LAUNCH(CFDETR_K_LN, launch_norm_residual(na, bf, bf, m_cap, s));
+    CF_LAUNCH(CFDETR_K_FF1, launch_gemm(ctx->o, mat(w.w_ff1, l * F * d), w.b_ff1 + l * F, (int)F, (int)d, Epilogue::kBiasGelu, ctx->h, nullptr,
+                                        bf, m_ptr, m_hint, m_cap, s, 1.0f, packed(ctx->slim_ff1, l * F * d)));
+    CF_LAUNCH(CFDETR_K_FF2, launch_gemm(ctx->h, mat(w.w_ff2, l * F * d), w.b_ff2 + l * d, (int)d, (int)F, Epilogue::kBias, ctx->a, nullptr, bf,
+                                        m_ptr, m_hint, m_cap, s, 1.0f, packed(ctx->slim_ff2, l * F * d)));
+    // behind the last layer the final LayerNorm, in fp32 to the caller's rows
+    na.post_g = f.post2_g ? f.post2_g + l * d : nullptr;
+    na.gate = f.gate2 ? f.gate2 + l * d : nullptr;
+    na.pre_g = last ? w.lnf_g : w.ln1_g + (l + 1) * d;
+    na.pre_b = last ? w.lnf_b : w.ln1_b + (l + 1) * d;
+    na.normed = last ? static_cast<void*>(y0) : ctx->a;
+    na.normed2 = last ? y1 : nullptr;
+    na.split_row = last ? split_row : 0;
+    CF_LAUNCH(CFDETR_K_LN, launch_norm_residual(na, bf, bf && !last, m_cap, s));
+  }
+  return CFDETR_OK;
+}
+
 // All layers + final LayerNorm over the tokens in ctx->x.  The sequences are
 // n_prefix coarse grids (n0 tokens each) followed by B sequences of the caller's; the
 // plan kernel, launched before, has turned that into ctx->cu_all / ctx->m_all, which every
 // kernel reads on the device, unless rows_known: m_cap then is the total, which saves every kernel that trip to memory
 // (a coarse pass of 920 rows, 39 such launches, 463 -> 456 us).  Output rows below split_row go to y0, the others to y1.
-cfdetr_status run_encoder(cfdetr_ctx* ctx, int nseq, const RunShape& shape, int m_cap, float* y0,
+cfdetr_status run_encoder(cfdetr_ctx* ctx, int nseq, const RunShape& shape, int m_cap, const RunCells& cells, float* y0,
                           int split_row, float* y1, hipStream_t s, const int32_t* kv_len = nullptr,
                           bool rows_known = false) {
+  if (ctx->has_diff) return run_differential(ctx, nseq, shape, m_cap, cells, y0, split_row, y1, s, kv_len, rows_known);
   const cfdetr_config& c = ctx->cfg;
   const cfdetr_weights& w = ctx->w;
   const int d = c.d_model, F = c.d_ffn;
@@ -641,7 +795,7 @@ cfdetr_status coarse_impl(cfdetr_ctx* ctx, const void* images, int B, float* x0_
   if (st != CFDETR_OK) return st;
   const RunShape shape = run_shape(ctx, RunKind::kExact, M, M);
   CF_LAUNCH(CFDETR_K_PLAN, launch_plan(ctx->coarse_cu, B, encoder_plan(ctx, 0, shape), s, M, ctx->err_flag));
-  return run_encoder(ctx, B, shape, M, y_coarse, 0, nullptr, s, nullptr, true);
+  return run_encoder(ctx, B, shape, M, {ctx->coarse_desc, M, nullptr}, y_coarse, 0, nullptr, s, nullptr, true);
 }
 
 cfdetr_status select_impl(cfdetr_ctx* ctx, const int32_t* boxes, const uint8_t* tier,
@@ -690,7 +844,7 @@ cfdetr_status fine_impl(cfdetr_ctx* ctx, const void* images, int B, const int32_
   CF_LAUNCH(CFDETR_K_PLAN, launch_plan(cu, B, encoder_plan(ctx, 0, shape), s, cap, ctx->err_flag));
   cfdetr_status st = fine_embed(ctx, images, B, tok_desc, ctx->cu_all, x0_cache, 0, s);
   if (st != CFDETR_OK) return st;
-  return run_encoder(ctx, B, shape, cap, y_mixed, 0, nullptr, s);
+  return run_encoder(ctx, B, shape, cap, {nullptr, 0, tok_desc}, y_mixed, 0, nullptr, s);
 }
 
 // A3 as the paper states it: every frame's token set brought to t_pad tokens (repeats of
@@ -708,7 +862,7 @@ cfdetr_status padded_impl(cfdetr_ctx* ctx, const void* images, int B, const int3
   cfdetr_status st = fine_embed(ctx, images, B, ctx->tok_pad, ctx->cu_pad, x0_cache, 0, s);
   if (st != CFDETR_OK) return st;
   CF_LAUNCH(CFDETR_K_PLAN, launch_plan(ctx->cu_pad, B, plan, s, B * t_pad, ctx->err_flag));
-  return run_encoder(ctx, B, shape, B * t_pad, y_padded, 0, nullptr, s, ctx->kv_len);
+  return run_encoder(ctx, B, shape, B * t_pad, {nullptr, 0, ctx->tok_pad}, y_padded, 0, nullptr, s, ctx->kv_len);
 }
 
 // The decoder's layers at widths 256 and 384: the encoder's kernels of those widths on the query rows, and
@@ -1034,7 +1188,7 @@ cfdetr_status merged_impl(cfdetr_ctx* ctx, const void* images, int B, const int3
   if (st != CFDETR_OK) return st;
   st = fine_embed(ctx, images, B, tok_desc, cu_seqlens, ctx->x0, Mc, s);
   if (st != CFDETR_OK) return st;
-  return run_encoder(ctx, 2 * B, shape, Mc + ctx->cfg.max_tokens_total, y_coarse, Mc, y_mixed, s);
+  return run_encoder(ctx, 2 * B, shape, Mc + ctx->cfg.max_tokens_total, {ctx->coarse_desc, Mc, tok_desc}, y_coarse, Mc, y_mixed, s);
 }
 
 }  // namespace
@@ -1262,6 +1416,7 @@ CFDETR_API void cfdetr_destroy(cfdetr_ctx* ctx) {
   if (ctx->m_seen) hipHostFree(ctx->m_seen);
   if (ctx->arena) hipFree(ctx->arena);
   if (ctx->dec_arena) hipFree(ctx->dec_arena);
+  if (ctx->diff_arena) hipFree(ctx->diff_arena);
   delete ctx;
 }
 
@@ -1596,6 +1751,199 @@ CFDETR_API cfdetr_status cfdetr_decode(cfdetr_ctx* ctx, const float* memory,
   if (!memory || !cu_seqlens || !queries) return fail(ctx, CFDETR_EINVAL, "null pointer");
   if (!aligned16(memory)) return fail(ctx, CFDETR_EINVAL, "memory must be 16-byte aligned");
   return decode_impl(ctx, memory, cu_seqlens, B, queries, static_cast<hipStream_t>(hip_stream));
+}
+
+CFDETR_API cfdetr_status cfdetr_rotary_frequencies(const cfdetr_rotary_params* params, double* freq) {
+  if (!params || !freq) return fail_create(CFDETR_EINVAL, "null pointer");
+  if (const char* why = check_rotary(*params, 64, true)) return fail_create(CFDETR_EINVAL, why);
+  rotary_frequencies(*params, freq);
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_params* params,
+                            const double* freq, const float* pos, int32_t M, const void* q,
+                            int32_t q_ld, void* q_out, int32_t q_out_ld, float q_scale,
+                            const void* k, int32_t k_ld, void* k_out, int32_t k_out_ld,
+                            void* hip_stream) {
+  cfdetr_status st = check_device(ctx);
+  if (st != CFDETR_OK) return st;
+  if (!params) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  const int dh = ctx->cfg.d_model / ctx->cfg.n_heads;
+  if (const char* why = check_rotary(*params, dh, false)) return fail(ctx, CFDETR_EINVAL, why);
+  if (M < 0) return fail(ctx, CFDETR_EINVAL, "M must be >= 0");
+  if (!std::isfinite(q_scale)) return fail(ctx, CFDETR_EINVAL, "q_scale is not a finite number");
+  if (!k != !k_out) return fail(ctx, CFDETR_EINVAL, "k and k_out go together");
+  if (M == 0) return CFDETR_OK;
+  if (!freq || !pos) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if (reinterpret_cast<uintptr_t>(freq) % 8 || reinterpret_cast<uintptr_t>(pos) % 4)
+    return fail(ctx, CFDETR_EINVAL, "frequencies or positions are not aligned");
+  const struct { const void* p; int ld; } rows[] = {{q, q_ld}, {q_out, q_out_ld}, {k, k_ld}, {k_out, k_out_ld}};
+  for (int i = 0; i < (k ? 4 : 2); ++i)
+    if (const char* why = check_rows(ctx, rows[i].p, rows[i].ld)) return fail(ctx, CFDETR_EINVAL, why);
+  if ((q == q_out && q_ld != q_out_ld) || (k && k == k_out && k_ld != k_out_ld))
+    return fail(ctx, CFDETR_EINVAL, "rows rotated in place keep their distance");
+  RotaryArgs a{};
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.qo_ld = q_out_ld;
+  a.ko_ld = k_out_ld;
+  a.pos = pos;
+  a.freq = freq;
+  a.m_capacity = M;
+  a.heads = ctx->cfg.n_heads;
+  a.d_head = dh;
+  a.rot_dim = params->rot_dim;
+  a.n_axes = params->n_axes;
+  a.interleaved = params->interleaved != 0;
+  a.q_scale = q_scale;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_QKV, launch_rotary(a, ctx->bf16, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_diff_attention(cfdetr_ctx* ctx, const void* q, int32_t q_ld, int32_t n_q,
+                                    const void* k, int32_t k_ld, const void* v, int32_t v_ld,
+                                    int32_t n_k, const int32_t* cu_q, const int32_t* cu_k,
+                                    int32_t B, const uint8_t* key_mask, const float* lambda,
+                                    const float* head_g, float softmax_scale, void* out,
+                                    int32_t out_ld, void* hip_stream) {
+  cfdetr_status st = check_call(ctx, B);
+  if (st != CFDETR_OK) return st;
+  const cfdetr_config& c = ctx->cfg;
+  if (c.n_heads % 2) return fail(ctx, CFDETR_ESHAPE, "differential attention needs an even n_heads");
+  if (n_q < 0 || n_k < 0) return fail(ctx, CFDETR_EINVAL, "row counts must be >= 0");
+  if (n_q > c.max_tokens_total || n_k > c.max_tokens_total)
+    return fail(ctx, CFDETR_ECAPACITY, "more rows than max_tokens_total");
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale))
+    return fail(ctx, CFDETR_EINVAL, "softmax_scale must be a number, at least 0");
+  if (!cu_q || !cu_k || !lambda) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if (!aligned16(head_g)) return fail(ctx, CFDETR_EINVAL, "head_g must be 16-byte aligned");
+  if (n_q == 0) return CFDETR_OK;
+  const struct { const void* p; int ld; } rows[] = {{q, q_ld}, {out, out_ld}, {k, k_ld}, {v, v_ld}};
+  for (int i = 0; i < (n_k ? 4 : 2); ++i)
+    if (const char* why = check_rows(ctx, rows[i].p, rows[i].ld)) return fail(ctx, CFDETR_EINVAL, why);
+  if (q == out && q_ld != out_ld) return fail(ctx, CFDETR_EINVAL, "rows written in place keep their distance");
+  DiffAttentionArgs a{};
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.v_ld = v_ld;
+  a.out_ld = out_ld;
+  a.n_q = n_q;
+  a.n_k = n_k;
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.B = B;
+  a.lambda = lambda;
+  a.head_g = head_g;
+  a.scale2 = softmax_scale > 0.f ? softmax_scale * 1.44269504088896340736f : 1.0f;
+  a.eps = c.ln_eps;
+  a.heads = c.n_heads / 2;
+  const int dh = c.d_model / c.n_heads;
+  a.splits = diff_attention_splits(n_q, n_k, B, a.heads, dh, partial_bytes(ctx), ctx->cus);
+  a.partial = static_cast<float*>(ctx->h);
+  a.err_flag = ctx->err_flag;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (key_mask && n_k) {
+    // (both are idle between the encode calls)
+    a.key_list = ctx->vt_pos;
+    a.kv_len = ctx->kv_len;
+    CF_LAUNCH(CFDETR_K_PLAN, launch_key_list(key_mask, cu_k, B, n_k, ctx->vt_pos, ctx->kv_len, s));
+  }
+  CF_LAUNCH(CFDETR_K_ATTN, launch_diff_attention(a, dh, ctx->bf16, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_norm_residual(cfdetr_ctx* ctx, const cfdetr_norm_residual_params* params,
+                                   const float* x, const void* block, float* x_out, void* normed,
+                                   int32_t M, void* hip_stream) {
+  cfdetr_status st = check_device(ctx);
+  if (st != CFDETR_OK) return st;
+  if (!params) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  const cfdetr_norm_residual_params& p = *params;
+  const struct { cfdetr_norm kind; const float *g, *b; } norms[] = {{p.post, p.post_g, p.post_b}, {p.pre, p.pre_g, p.pre_b}};
+  for (const auto& n : norms) {
+    if (n.kind != CFDETR_NORM_NONE && n.kind != CFDETR_NORM_LAYER && n.kind != CFDETR_NORM_RMS)
+      return fail(ctx, CFDETR_EINVAL, "no such norm");
+    if ((n.kind == CFDETR_NORM_NONE) != !n.g || (n.b && n.kind != CFDETR_NORM_LAYER))
+      return fail(ctx, CFDETR_EINVAL, "a norm has a gain, and only a LayerNorm an offset");
+    if (!aligned16(n.g) || !aligned16(n.b)) return fail(ctx, CFDETR_EINVAL, "pointers must be 16-byte aligned");
+  }
+  if (!std::isfinite(p.res_scale)) return fail(ctx, CFDETR_EINVAL, "res_scale is not a finite number");
+  if (p.cu_seqlens && !p.gate) return fail(ctx, CFDETR_EINVAL, "offsets without a gate");
+  if (p.cu_seqlens)
+    if (st = check_call(ctx, p.B); st != CFDETR_OK) return st;
+  if (M < 0) return fail(ctx, CFDETR_EINVAL, "M must be >= 0");
+  if (M == 0) return CFDETR_OK;
+  if (!x || !block || !x_out) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if ((p.pre == CFDETR_NORM_NONE) != !normed) return fail(ctx, CFDETR_EINVAL, "normed goes with the norm in front of the next block");
+  if (!aligned16(x) || !aligned16(block) || !aligned16(x_out) || !aligned16(normed) || !aligned16(p.gate))
+    return fail(ctx, CFDETR_EINVAL, "pointers must be 16-byte aligned");
+  NormResidualArgs a{};
+  a.x = x;
+  a.block = block;
+  a.x_out = x_out;
+  a.normed = normed;
+  a.post = static_cast<NormKind>(p.post);
+  a.pre = static_cast<NormKind>(p.pre);
+  a.post_g = p.post_g;
+  a.post_b = p.post_b;
+  a.pre_g = p.pre_g;
+  a.pre_b = p.pre_b;
+  a.gate = p.gate;
+  a.cu = p.cu_seqlens;
+  a.B = p.B;
+  a.res_scale = p.res_scale;
+  a.eps = ctx->cfg.ln_eps;
+  a.d = ctx->cfg.d_model;
+  a.err_flag = ctx->err_flag;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_LN, launch_norm_residual(a, ctx->bf16, ctx->bf16, M, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdetr_differential_weights* w) {
+  cfdetr_status st = check_device(ctx);
+  if (st != CFDETR_OK) return st;
+  if (!w) return fail(ctx, CFDETR_EINVAL, "null argument");
+  if (ctx->has_diff) return fail(ctx, CFDETR_EINVAL, "the context already has layers of the differential form");
+  const cfdetr_config& c = ctx->cfg;
+  if (c.n_heads % 2) return fail(ctx, CFDETR_ESHAPE, "differential attention needs an even n_heads");
+  if (!w->lambda || !w->post1_g != !w->post2_g || !w->gate1 != !w->gate2)
+    return fail(ctx, CFDETR_EINVAL, "null weight, or one of a pair");
+  for (const void* p : {w->lambda, w->head_g, w->post1_g, w->post2_g, w->gate1, w->gate2})
+    if (!aligned16(p)) return fail(ctx, CFDETR_EINVAL, "misaligned weight");
+  if (!std::isfinite(w->res_scale)) return fail(ctx, CFDETR_EINVAL, "res_scale is not a finite number");
+  if (const char* why = check_rotary(w->rotary, c.d_model / c.n_heads, true)) return fail(ctx, CFDETR_EINVAL, why);
+  if (w->rotary.n_axes != 2) return fail(ctx, CFDETR_EINVAL, "cells have two coordinates");
+  Carver cv;
+  const uint64_t o_freq = cv.take(sizeof(double) * (w->rotary.rot_dim / 2)), o_pos = cv.take(ctx->tok_cap * 2 * sizeof(float));
+  hipError_t e = hipMalloc(&ctx->diff_arena, cv.off);
+  if (e != hipSuccess) {
+    ctx->diff_arena = nullptr;
+    return fail(ctx, CFDETR_ENOMEM, "hipMalloc of the differential layers' work space");
+  }
+  char* base = static_cast<char*>(ctx->diff_arena);
+  double freq[32];
+  rotary_frequencies(w->rotary, freq);
+  e = hipMemcpy(base + o_freq, freq, sizeof(double) * (w->rotary.rot_dim / 2), hipMemcpyHostToDevice);
+  if (e != hipSuccess) {
+    hipFree(ctx->diff_arena);
+    ctx->diff_arena = nullptr;
+    return fail_hip(ctx, "differential layers' set-up", e);
+  }
+  ctx->diff_freq = reinterpret_cast<double*>(base + o_freq);
+  ctx->diff_pos = reinterpret_cast<float*>(base + o_pos);
+  ctx->fw = *w;
+  ctx->has_diff = true;
+  return CFDETR_OK;
 }
 
 CFDETR_API cfdetr_status cfdetr_profile_begin(cfdetr_ctx* ctx) {

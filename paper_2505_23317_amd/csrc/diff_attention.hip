@@ -1,0 +1,532 @@
+// Differential attention (operator of a differential encoder layer) over variable-length sequences.
+//
+// Head h has two query / key heads of width dh (2h and 2h + 1 of the rows) and values of width 2 dh:
+//   A_m = softmax over the frame's keys of scale q_m k_m^T, m = 1, 2;   o = (A_1 - lambda_h A_2) v
+// and, with a gain, o <- o / sqrt(mean(o^2) + eps) * gain.  A frame without keys gives rows of zeros.
+#include <algorithm>
+#include <type_traits>
+
+#include "kernels.h"
+
+namespace cfdetr {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnitKeys = 32;   // keys of one step of a wavefront
+constexpr int kTileQ = 32;      // queries of a workgroup (a lane each)
+
+__device__ __forceinline__ int swap_bits_2_3(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+// Where the frames of a batch lie: lane l of every wavefront holds the offsets of frames 2l and 2l + 1
+// (the merged run of the encoder has two sequences for each of up to 64 cameras).
+struct Frames {
+  int q[3], k[3];
+  bool bad;   // a negative length, or an end beyond the rows: the whole call is refused
+};
+__device__ __forceinline__ Frames frames_of(const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k, int B, int n_q, int n_k) {
+  const int l = 2 * (threadIdx.x & 63);
+  Frames f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    f.q[i] = cu_q[min(l + i, B)];
+    f.k[i] = cu_k[min(l + i, B)];
+    bad |= f.q[i] < 0 || f.k[i] < 0 || f.q[i] > n_q || f.k[i] > n_k || (i > 0 && (f.q[i] < f.q[i - 1] || f.k[i] < f.k[i - 1]));
+  }
+  f.bad = __any(bad || (l == 0 && (f.q[0] != 0 || f.k[0] != 0)));
+  return f;
+}
+// The frame that piece `id` belongs to, where a frame has pieces[0 or 1] of them (lane's two frames); `id` becomes
+// the piece's number within it.  -1: there are fewer.
+__device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int& id) {
+  const int lane = threadIdx.x & 63;
+  int upto = pieces[0] + pieces[1];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o);
+    if (lane >= o) upto += v;
+  }
+  const uint64_t in = __ballot(upto > id);
+  if (in == 0) return -1;
+  const int l = __ffsll((unsigned long long)in) - 1;
+  const int first = __builtin_amdgcn_readlane(pieces[0], l);
+  id -= __builtin_amdgcn_readlane(upto, l) - first - __builtin_amdgcn_readlane(pieces[1], l);
+  if (id < first) return 2 * l;
+  id -= first;
+  return 2 * l + 1;
+}
+__device__ __forceinline__ int of_frame(const int (&offsets)[3], int frame) {
+  return __builtin_amdgcn_readlane((frame & 1) ? offsets[1] : offsets[0], frame >> 1);
+}
+__device__ __forceinline__ int behind_frame(const int (&offsets)[3], int frame) {
+  return __builtin_amdgcn_readlane((frame & 1) ? offsets[2] : offsets[1], frame >> 1);
+}
+
+// ---- elements --------------------------------------------------------------------------
+// bf16: operands of 32x32x16 products, 8 elements a lane and step.  fp32: of 32x32x2 products, one.
+// In both, an operand row in LDS or memory is cut into chunks of 16 bytes and a lane of group g (lanes 32 g on)
+// has chunk 2c + g of chunk pair c.  S^T = K Q^T leaves a lane with 16 keys of one query.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<bf16_t> {
+  static constexpr int kChunk = 8;   // elements of 16 bytes
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ f32x16 dot(const uint4& k, const uint4& q, f32x16 acc) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&k), *reinterpret_cast<const bf16x8*>(&q), acc, 0, 0, 0);
+  }
+  // LDS row of a key, so that eight consecutive result registers of a lane are eight consecutive keys
+  static __device__ __forceinline__ int row_of_key(int key) { return swap_bits_2_3(key); }
+  // key of result register r of lane group g
+  static __device__ __forceinline__ int key_of(int r, int g) { return 16 * (r >> 3) + 8 * g + (r & 7); }
+};
+template <>
+struct Elem<float> {
+  static constexpr int kChunk = 4;
+  static __device__ __forceinline__ f32x16 dot(const uint4& k, const uint4& q, f32x16 acc) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.x), __uint_as_float(q.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.y), __uint_as_float(q.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.z), __uint_as_float(q.z), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.w), __uint_as_float(q.w), acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ int row_of_key(int key) { return key; }
+  static __device__ __forceinline__ int key_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
+};
+
+// Order of a row's chunks in LDS.  Keys: 16 rows that are read together lie in all banks.  Values: blocks of 32
+// columns, moved so that the rows a product reads together lie in different banks.
+template <typename T, int ROWB>
+__device__ __forceinline__ int key_chunk(int row, int c) {
+  return ROWB == 128 ? c ^ ((row >> 1) & 7) : c ^ (row & 15);
+}
+template <typename T, int ROWB>
+__device__ __forceinline__ int value_block(int row, int b) {
+  if constexpr (std::is_same_v<T, float>) return b ^ ((row >> 2) & 1);
+  return ROWB == 128 ? b ^ ((row >> 1) & 1) : b ^ (row & 3);
+}
+
+// Sum of v over the lanes l and l ^ 32, and the larger of the two.
+__device__ __forceinline__ float half_sum(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float half_max(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row16(T* to, const float (&x)[16]);
+template <>
+__device__ __forceinline__ void store_row16<bf16_t>(bf16_t* to, const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<uint4*>(to)[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
+                                                 pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
+}
+template <>
+__device__ __forceinline__ void store_row16<float>(float* to, const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(to)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_row8(T* to, const float (&x)[8]);
+template <>
+__device__ __forceinline__ void store_row8<bf16_t>(bf16_t* to, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+template <>
+__device__ __forceinline__ void store_row8<float>(float* to, const float (&x)[8]) {
+  reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// ---- few queries, or fp32 ----------------------------------------------------------------
+// A workgroup has 32 queries of one head and frame and one of `splits` runs of its keys; its four wavefronts take
+// units of 32 keys in turn, each with a running maximum and sum of both maps, through LDS of its own, so that
+// there is no barrier before the end.  There the four partial results are brought to one maximum and added up in LDS.
+// splits > 1: row, head and split leave their maxima, sums and unscaled rows in `partial`, which
+// diff_join_kernel adds up in a fixed order.
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs a) {
+  constexpr int W = 2 * DH;                         // columns of both keys of a head, and of its values
+  constexpr int ROWB = W * (int)sizeof(T);          // bytes of such a row
+  constexpr int CPR = ROWB / 16;                    // chunks of it
+  constexpr int KS = CPR / 4;                       // chunk pairs of one map
+  constexpr int MO = W / 32;                        // blocks of 32 output columns
+  constexpr int LI = kUnitKeys * CPR / 64;          // chunks of a unit's keys (and of its values) a lane
+  constexpr int UNIT = kUnitKeys * ROWB;
+  constexpr int WAVE = 2 * UNIT > 2 * 32 * W * 4 ? 2 * UNIT : 2 * 32 * W * 4;   // LDS of a wavefront: keys and values, then its two maps' rows
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ float s_m[4][2][32], s_l[4][2][32];
+
+  const Frames fr = frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k);
+  if (fr.bad) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.err_flag = 1;
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.heads;
+  int tile = blockIdx.x / a.splits / a.heads;
+  const int tiles[2] = {(fr.q[1] - fr.q[0] + kTileQ - 1) / kTileQ, (fr.q[2] - fr.q[1] + kTileQ - 1) / kTileQ};
+  const int frame = frame_of_piece(tiles, tile);
+  if (frame < 0) return;
+  const int q0 = of_frame(fr.q, frame), nq = behind_frame(fr.q, frame) - q0;
+  const int k0 = of_frame(fr.k, frame), nk_all = behind_frame(fr.k, frame) - k0;
+  const int nk = a.kv_len ? min(nk_all, a.kv_len[frame]) : nk_all;
+  const int units = (nk + kUnitKeys - 1) / kUnitKeys, share = (units + a.splits - 1) / a.splits;
+  const int u_end = min(units, (split + 1) * share);
+
+  const T* const kbase = static_cast<const T*>(a.k) + (size_t)k0 * a.k_ld + head * W;
+  const T* const vbase = static_cast<const T*>(a.v) + (size_t)k0 * a.v_ld + head * W;
+  const int32_t* const list = a.key_list ? a.key_list + k0 : nullptr;
+  unsigned char* const sK = smem + wave * WAVE;
+  unsigned char* const sV = sK + UNIT;
+
+  uint4 qf[2][KS];
+  {
+    const int row = min(tile * kTileQ + l32, nq - 1);
+    const T* const qrow = static_cast<const T*>(a.q) + (size_t)(q0 + row) * a.q_ld + head * W;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int c = 0; c < KS; ++c) qf[m][c] = *reinterpret_cast<const uint4*>(qrow + m * DH + (2 * c + g) * Elem<T>::kChunk);
+  }
+  uint4 kr[LI], vr[LI];
+  auto fetch = [&](int u) {   // a unit's keys and values; past the last key zeros
+#pragma unroll
+    for (int j = 0; j < LI; ++j) {
+      const int p = 64 * j + lane, key = p / CPR, c = p % CPR, at = u * kUnitKeys + key;
+      kr[j] = vr[j] = make_uint4(0, 0, 0, 0);
+      if (at < nk) {
+        const size_t row = list ? list[at] : at;
+        kr[j] = *reinterpret_cast<const uint4*>(kbase + row * a.k_ld + c * Elem<T>::kChunk);
+        vr[j] = *reinterpret_cast<const uint4*>(vbase + row * a.v_ld + c * Elem<T>::kChunk);
+      }
+    }
+  };
+  f32x16 acc[2][MO];
+  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int i = 0; i < MO; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[m][i][r] = 0.f;
+
+  int u = split * share + wave;
+  if (u < u_end) fetch(u);
+#pragma nounroll
+  for (; u < u_end; u += 4) {
+    wave_fence();
+#pragma unroll
+    for (int j = 0; j < LI; ++j) {
+      const int p = 64 * j + lane, key = p / CPR, c = p % CPR, row = Elem<T>::row_of_key(key);
+      *reinterpret_cast<uint4*>(sK + row * ROWB + key_chunk<T, ROWB>(row, c) * 16) = kr[j];
+      constexpr int CPB = 32 * (int)sizeof(T) / 16;   // chunks of a block of 32 columns
+      *reinterpret_cast<uint4*>(sV + key * ROWB + (value_block<T, ROWB>(key, c / CPB) * CPB + c % CPB) * 16) = vr[j];
+    }
+    if (u + 4 < u_end) fetch(u + 4);
+    wave_fence();
+    f32x16 s[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        s[m] = Elem<T>::dot(*reinterpret_cast<const uint4*>(sK + l32 * ROWB + key_chunk<T, ROWB>(l32, m * 2 * KS + 2 * c + g) * 16),
+                            qf[m][c], s[m]);
+      const int left = nk - u * kUnitKeys;
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[m][r] = Elem<T>::key_of(r, g) < left ? s[m][r] * a.scale2 : -INFINITY;
+        top = fmaxf(top, s[m][r]);
+      }
+      const float m_new = fmaxf(m_run[m], half_max(top));
+      const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run[m] - m_ref);
+      m_run[m] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[m][r] = __builtin_amdgcn_exp2f(s[m][r] - m_ref);
+        sum += s[m][r];
+      }
+      l_run[m] = l_run[m] * alpha + sum;
+#pragma unroll
+      for (int i = 0; i < MO; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[m][i][r] *= alpha;
+    }
+    if constexpr (std::is_same_v<T, bf16_t>) {
+      // A rounding of the probabilities to bf16: half a step of 2^-8 each, independent between keys.
+      typedef __attribute__((ext_vector_type(4))) short s16x4;
+      typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        bf16x8 p[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          uint4 w = make_uint4(pack_bf16x2(s[m][8 * t], s[m][8 * t + 1]), pack_bf16x2(s[m][8 * t + 2], s[m][8 * t + 3]),
+                               pack_bf16x2(s[m][8 * t + 4], s[m][8 * t + 5]), pack_bf16x2(s[m][8 * t + 6], s[m][8 * t + 7]));
+          p[m] = *reinterpret_cast<bf16x8*>(&w);
+        }
+#pragma unroll
+        for (int i = 0; i < MO; ++i) {
+          // values come row by row; the transposing read gives a lane four keys of its column, a group of 16 lanes
+          // naming the pieces of four keys by 16 columns
+          union {
+            s16x4 half[2];
+            bf16x8 whole;
+          } v;
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const int key = 16 * t + 8 * g + 4 * hh + ((lane & 15) >> 2);
+            v.half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds4)(sV + key * ROWB + value_block<T, ROWB>(key, i) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8));
+          }
+#pragma unroll
+          for (int m = 0; m < 2; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.whole, p[m], acc[m][i], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = Elem<T>::key_of(r, g);
+#pragma unroll
+        for (int i = 0; i < MO; ++i) {
+          const float v = *reinterpret_cast<const float*>(sV + key * ROWB + value_block<T, ROWB>(key, i) * 128 + l32 * 4);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[m][r], acc[m][i], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // The four wavefronts' results to one maximum, and into LDS: row of a query, its quads of columns moved by the query.
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    l_run[m] = half_sum(l_run[m]);
+    if (g == 0) {
+      s_m[wave][m][l32] = m_run[m];
+      s_l[wave][m][l32] = l_run[m];
+    }
+  }
+  __syncthreads();
+  float top[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    top[m] = fmaxf(fmaxf(s_m[0][m][l32], s_m[1][m][l32]), fmaxf(s_m[2][m][l32], s_m[3][m][l32]));
+    const float f = __builtin_amdgcn_exp2f(m_run[m] - (top[m] == -INFINITY ? 0.f : top[m]));
+    float* const rows = reinterpret_cast<float*>(sK) + m * 32 * W + l32 * W;
+#pragma unroll
+    for (int i = 0; i < MO; ++i)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        const int quad = 8 * i + 2 * rq + g;   // columns 32 i + 8 rq + 4 g on
+        *reinterpret_cast<float4*>(rows + 4 * (quad ^ (l32 & (W / 4 - 1)))) =
+            make_float4(acc[m][i][4 * rq] * f, acc[m][i][4 * rq + 1] * f, acc[m][i][4 * rq + 2] * f, acc[m][i][4 * rq + 3] * f);
+      }
+  }
+  __syncthreads();
+  // thread: query tid / 8, an eighth of its columns
+  constexpr int CE = W / 8;
+  const int qi = tid >> 3, part = tid & 7;
+  const int q_local = tile * kTileQ + qi;
+  float o[2][CE], l_all[2], m_all[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    m_all[m] = fmaxf(fmaxf(s_m[0][m][qi], s_m[1][m][qi]), fmaxf(s_m[2][m][qi], s_m[3][m][qi]));
+    l_all[m] = 0.f;
+#pragma unroll
+    for (int e = 0; e < CE; ++e) o[m][e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      l_all[m] += s_l[w][m][qi] * __builtin_amdgcn_exp2f(s_m[w][m][qi] - (m_all[m] == -INFINITY ? 0.f : m_all[m]));
+      const float* const rows = reinterpret_cast<const float*>(smem + w * WAVE) + m * 32 * W + qi * W;
+#pragma unroll
+      for (int e = 0; e < CE / 4; ++e) {
+        const float4 v = *reinterpret_cast<const float4*>(rows + 4 * ((part * (CE / 4) + e) ^ (qi & (W / 4 - 1))));
+        o[m][4 * e] += v.x;
+        o[m][4 * e + 1] += v.y;
+        o[m][4 * e + 2] += v.z;
+        o[m][4 * e + 3] += v.w;
+      }
+    }
+  }
+  if (a.splits > 1) {
+    if (q_local < nq) {
+      float* const to = a.partial + (((size_t)(q0 + q_local) * a.heads + head) * a.splits + split) * (2 * W + 4);
+      if (part == 0) *reinterpret_cast<float4*>(to) = make_float4(m_all[0], m_all[1], l_all[0], l_all[1]);
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < CE / 4; ++e)
+          *reinterpret_cast<float4*>(to + 4 + m * W + part * CE + 4 * e) = make_float4(o[m][4 * e], o[m][4 * e + 1], o[m][4 * e + 2], o[m][4 * e + 3]);
+    }
+    return;
+  }
+  const float i0 = l_all[0] != 0.f ? 1.0f / l_all[0] : 0.f, i1 = l_all[1] != 0.f ? a.lambda[head] / l_all[1] : 0.f;
+  float x[CE], sq = 0.f;
+#pragma unroll
+  for (int e = 0; e < CE; ++e) {
+    x[e] = o[0][e] * i0 - o[1][e] * i1;
+    sq = fmaf(x[e], x[e], sq);
+  }
+  if (a.head_g) {
+#pragma unroll
+    for (int s = 1; s < 8; s <<= 1) sq += __shfl_xor(sq, s);
+    const float r = rsqrtf(sq * (1.0f / W) + a.eps);
+#pragma unroll
+    for (int e = 0; e < CE; ++e) x[e] *= r * a.head_g[part * CE + e];
+  }
+  if (q_local < nq) {
+    T* const to = static_cast<T*>(a.out) + (size_t)(q0 + q_local) * a.out_ld + head * W + part * CE;
+    if constexpr (CE == 16) store_row16<T>(to, x);
+    else store_row8<T>(to, x);
+  }
+}
+
+// The splits' results of a row and head, by one wavefront: lane's quad of columns of map lane / 32, in split order.
+template <typename T, int DH>
+__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffAttentionArgs a) {
+  constexpr int W = 2 * DH, Q = W / 4;   // quads of a map: 32 or 16 lanes of its 32
+  if (frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad) return;
+  const int lane = threadIdx.x & 63, map = lane >> 5, quad = lane & 31;
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = item / a.heads, head = item - row * a.heads;
+  if (row >= a.cu_q[a.B]) return;
+  const float* const from = a.partial + (size_t)item * a.splits * (2 * W + 4);
+  float m = -INFINITY;
+  for (int s = lane & 31; s < a.splits; s += 32) m = fmaxf(m, from[(size_t)s * (2 * W + 4) + map]);
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
+  const float m_ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < a.splits; ++s) {
+    const float* const p = from + (size_t)s * (2 * W + 4);
+    const float f = __builtin_amdgcn_exp2f(p[map] - m_ref);
+    l = fmaf(p[2 + map], f, l);
+    if (quad < Q) {
+      const float4 v = *reinterpret_cast<const float4*>(p + 4 + map * W + 4 * quad);
+      o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
+    }
+  }
+  const float i = l != 0.f ? (map ? -a.lambda[head] : 1.0f) / l : 0.f;
+  o = make_float4(half_sum(o.x * i), half_sum(o.y * i), half_sum(o.z * i), half_sum(o.w * i));
+  if (a.head_g) {
+    float sq = fmaf(o.x, o.x, o.y * o.y) + fmaf(o.z, o.z, o.w * o.w);
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) sq += __shfl_xor(sq, s);
+    const float r = rsqrtf(sq * (1.0f / W) + a.eps);
+    if (quad < Q) {
+      const float4 gq = *reinterpret_cast<const float4*>(a.head_g + 4 * quad);
+      o = make_float4(o.x * r * gq.x, o.y * r * gq.y, o.z * r * gq.z, o.w * r * gq.w);
+    }
+  }
+  if (map == 0 && quad < Q) {
+    T* const to = static_cast<T*>(a.out) + (size_t)row * a.out_ld + head * W + 4 * quad;
+    if constexpr (std::is_same_v<T, float>)
+      *reinterpret_cast<float4*>(to) = o;
+    else
+      *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+  }
+}
+
+// ---- masked keys ---------------------------------------------------------------------------
+// The keys of every frame that its mask leaves, in order, as row numbers within the frame, and their count: masked
+// rows are then never read.  A workgroup lists kListKeys keys of one frame, after it has counted those before.
+constexpr int kListKeys = 2048;
+__global__ __launch_bounds__(kThreads) void key_list_kernel(const uint8_t* __restrict__ mask, const int32_t* __restrict__ cu_k,
+                                                            int B, int n_k, int32_t* __restrict__ list, int32_t* __restrict__ kv_len) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Frames fr = frames_of(cu_k, cu_k, B, n_k, n_k);
+  if (fr.bad) return;   // refused by the attention
+  const int parts[2] = {lane * 2 < B ? max(1, (fr.k[1] - fr.k[0] + kListKeys - 1) / kListKeys) : 0,
+                        lane * 2 + 1 < B ? max(1, (fr.k[2] - fr.k[1] + kListKeys - 1) / kListKeys) : 0};
+  int part = blockIdx.x;
+  const int f = frame_of_piece(parts, part);
+  if (f < 0) return;
+  const int k0 = of_frame(fr.k, f), nk = behind_frame(fr.k, f) - k0;
+  const int first = part * kListKeys, end = min(nk, first + kListKeys);
+  const uint8_t* const m = mask + k0;
+  __shared__ int s_count[4];
+  int before = 0;
+#pragma unroll 8
+  for (int i = tid; i < first; i += kThreads) before += m[i] != 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) before += __shfl_xor(before, o);
+  if (lane == 0) s_count[wave] = before;
+  __syncthreads();
+  int at = s_count[0] + s_count[1] + s_count[2] + s_count[3];
+  // this part: a wavefront's keys are consecutive, 64 a step
+  constexpr int STEPS = kListKeys / kThreads;
+  uint64_t bits[STEPS];
+  int mine = 0;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int i = first + (wave * STEPS + s) * 64 + lane;
+    bits[s] = __ballot(i < end && m[i] != 0);
+    mine += __popcll(bits[s]);
+  }
+  __syncthreads();
+  if (lane == 0) s_count[wave] = mine;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) at += s_count[w];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    if (bits[s] >> lane & 1) list[k0 + at + __popcll(bits[s] & ((uint64_t(1) << lane) - 1))] = first + (wave * STEPS + s) * 64 + lane;
+    at += __popcll(bits[s]);
+  }
+  if (end == nk && wave == 3 && lane == 0) kv_len[f] = at;
+}
+
+template <typename T, int DH>
+hipError_t few(const DiffAttentionArgs& a, hipStream_t s) {
+  constexpr int W = 2 * DH, UNIT = kUnitKeys * W * (int)sizeof(T);
+  constexpr int WAVE = 2 * UNIT > 2 * 32 * W * 4 ? 2 * UNIT : 2 * 32 * W * 4;
+  static DeviceOnce once;
+  if (hipError_t e = allow_lds(diff_few_kernel<T, DH>, 4 * WAVE, &once); e != hipSuccess) return e;
+  const int64_t grid = ((int64_t)a.n_q / kTileQ + a.B) * a.heads * a.splits;
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((diff_few_kernel<T, DH>), dim3((unsigned)grid), dim3(kThreads), 4 * WAVE, s, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL((diff_join_kernel<T, DH>), dim3((unsigned)(((int64_t)a.n_q * a.heads + 3) / 4)), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int n_k, int32_t* list, int32_t* kv_len, hipStream_t s) {
+  hipLaunchKernelGGL(key_list_kernel, dim3(n_k / kListKeys + B), dim3(kThreads), 0, s, mask, cu_k, B, n_k, list, kv_len);
+  return hipGetLastError();
+}
+
+int diff_attention_splits(int n_q, int n_k, int B, int heads, int d_head, uint64_t partial_bytes, int cus) {
+  const int64_t tiles = (int64_t)B * ((n_q + (int64_t)B * kTileQ - 1) / ((int64_t)B * kTileQ)) * heads;
+  const int64_t units = (n_k / B + kUnitKeys - 1) / kUnitKeys;
+  const int64_t row = (int64_t)n_q * heads * (4 * d_head + 4) * 4;
+  int64_t splits = std::min<int64_t>({2 * cus / std::max<int64_t>(1, tiles), units / 8, (int64_t)(partial_bytes / std::max<int64_t>(1, row)), 128});
+  return (int)std::max<int64_t>(1, splits);
+}
+
+hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s) {
+  if (d_head == 64) return use_bf16 ? few<bf16_t, 64>(a, s) : few<float, 64>(a, s);
+  if (d_head == 32) return use_bf16 ? few<bf16_t, 32>(a, s) : few<float, 32>(a, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace cfdetr

@@ -423,4 +423,70 @@ int attention_block_q(int d_head, bool use_bf16, int64_t rows, int heads);
 // 0 if the device cannot be queried.
 int attention_grid(int d_head, bool use_bf16, int block_q, int cap8);
 
+// ---- differential encoder layers (rotary.hip, diff_attention.hip, norm_residual.hip) --------
+// Rows [M, ld] of queries and (k not null) keys, `heads` heads of d_head each, M = *m_ptr if
+// m_ptr else m_capacity; pos [M, n_axes], freq [rot_dim / 2] (device, 64 bits).  The outputs may be the inputs.
+struct RotaryArgs {
+  const void *q, *k;
+  void *q_out, *k_out;
+  int q_ld, k_ld, qo_ld, ko_ld;
+  const float* pos;
+  const double* freq;
+  const int32_t* m_ptr;
+  int m_capacity;
+  int heads, d_head, rot_dim, n_axes;
+  bool interleaved;
+  float q_scale;
+};
+hipError_t launch_rotary(const RotaryArgs& a, bool use_bf16, hipStream_t s);
+// pos[m] (two floats) = (row, column) of the centre of row m's cell in cells of the finest level; rows below n_first are
+// described by first[m], the others by second[m - n_first].
+hipError_t launch_cell_positions(const int32_t* first, int n_first, const int32_t* second, int finest, const int32_t* m_ptr,
+                                 int m_capacity, float* pos, hipStream_t s);
+
+// Differential attention of the rows of B <= 64 frames (cu_q) over those of the same frames (cu_k), the first kv_len[f] of
+// them where it is given, the kv_len[f] that key_list names (rows within the frame, from cu_k[f] on) where that is
+// given too.  Offsets that are none set *err_flag and nothing is written.  partial: room for
+// diff_attention_splits' partial results (splits > 1).  Logits are scaled by scale2 in base 2.
+struct DiffAttentionArgs {
+  const void *q, *k, *v;
+  void* out;
+  int q_ld, k_ld, v_ld, out_ld;
+  int n_q, n_k;
+  const int32_t *cu_q, *cu_k;
+  int B;
+  const int32_t *kv_len, *key_list;
+  const float *lambda, *head_g;
+  float scale2, eps;
+  int heads;   // differential heads
+  int splits;
+  float* partial;
+  int32_t* err_flag;
+};
+hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
+int diff_attention_splits(int n_q, int n_k, int B, int heads, int d_head, uint64_t partial_bytes, int cus);
+// list, kv_len: the keys of every frame whose mask byte is not 0, for launch_diff_attention.
+hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int n_k, int32_t* list, int32_t* kv_len, hipStream_t s);
+
+// x_out = res_scale x + gate * post(block);  normed = pre(x_out), for rows < M (M = *m_ptr if m_ptr else the capacity).
+// gate: null, [d], or with cu (B + 1 offsets) [B, d], one for every frame, and the rows behind the
+// last frame are left alone.  Rows from split_row on of normed go to normed2 where that is given.
+enum class NormKind { kNone = 0, kLayer = 1, kRms = 2 };
+struct NormResidualArgs {
+  const float* x;
+  const void* block;
+  float* x_out;
+  void *normed, *normed2;
+  int split_row;
+  NormKind post, pre;
+  const float *post_g, *post_b, *pre_g, *pre_b, *gate;
+  const int32_t* cu;
+  int B;
+  float res_scale, eps;
+  int d;
+  const int32_t* m_ptr;
+  int32_t* err_flag;
+};
+hipError_t launch_norm_residual(const NormResidualArgs& a, bool block_is_bf16, bool normed_is_bf16, int m_capacity, hipStream_t s);
+
 }  // namespace cfdetr
