@@ -433,7 +433,7 @@ CFDETR_API cfdetr_status cfdetr_decode(cfdetr_ctx* ctx, const float* memory,
  * form of this library's encoder that is made of them.  They take their shape from the context:
  * d = d_model columns, n_heads heads of d_head = d_model / n_heads, elements ("act") of act_dtype,
  * eps = ln_eps.  Rows of act lie `ld` elements apart; a pointer to act rows, and ld times the element's
- * size, are multiples of 16 bytes and ld >= d (else CFDETR_EINVAL).  Rows are never copied or
+ * size, are multiples of 16 bytes and d <= ld <= 2^24 (else CFDETR_EINVAL).  Rows are never copied or
  * moved; an output overlaps an input only where that is said.  The operators use the context's work
  * space: the rule that calls on one context must not overlap holds for them as for the others.
  */
@@ -487,7 +487,9 @@ CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_para
  * of n_heads / 2 has the query and key heads 2h and 2h + 1 and the values of width 2 d_head
  * that lie in the columns of both.  With A_1 and A_2 the softmax over the frame's keys of
  * softmax_scale q k^T of the two, a row is (A_1 - lambda[h] A_2) v, and with head_g
- * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.
+ * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.  The two maps'
+ * products with v are taken apart: a v that is not finite leaves NaN in its column of the frame's
+ * rows (lambda[h] = 0: what the first map makes of it).
  *   q [n_q, ld], k and v [n_k, ld] act; n_q, n_k <= max_tokens_total (else CFDETR_ECAPACITY)
  *   cu_q, cu_k  [B+1] int32 device: offsets of the frames' rows, from 0; frames may be empty.
  *               Negative lengths, or an end beyond n_q or n_k, make the call write nothing, and

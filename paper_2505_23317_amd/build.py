@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcfdetr.so")
 SOURCES = ["api.hip", "select.hip", "roi.hip", "rowwise.hip", "gemm.hip", "layer.hip", "small_layer.hip",
-           "few_rows.hip", "attention.hip", "sched.hip", "rotary.hip", "diff_attention.hip", "norm_residual.hip"]
+           "few_rows.hip", "attention.hip", "sched.hip", "rotary.hip", "diff_attention.hip", "diff_tiles.hip",
+           "norm_residual.hip"]
 # A kernel's first 14 words of arguments come in scalar registers with the launch, so that its first
 # loads need not wait for a load of their addresses (arguments that are structs are left in memory).
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hidden",
@@ -19,7 +20,8 @@ FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hi
 # Per-source extras.  The attention kernel reads every MFMA result back for the
 # softmax, so its accumulators should live in ordinary VGPRs (no AGPR copies); the
 # GEMMs only read theirs in the epilogue and are faster with AGPR accumulators.
-EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "diff_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:

@@ -242,10 +242,11 @@ void rotary_frequencies(const cfdetr_rotary_params& p, double* freq) {
   }
 }
 
-// Rows of act elements that an operator reads or writes.
+// Rows of act elements that an operator reads or writes; 32 of them are addressed with 32 bits.
+constexpr int kMaxRowElements = 1 << 24;
 const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld) {
   if (!p) return "null pointer";
-  if (ld < ctx->cfg.d_model) return "rows are shorter than d_model";
+  if (ld < ctx->cfg.d_model || ld > kMaxRowElements) return "rows must be d_model to 2^24 elements apart";
   if (!aligned16(p) || (size_t)ld * ctx->esz % 16) return "rows must begin on multiples of 16 bytes";
   return nullptr;
 }
@@ -450,7 +451,8 @@ cfdetr_status run_differential(cfdetr_ctx* ctx, int nseq, const RunShape& shape,
   aa.eps = c.ln_eps;
   aa.heads = c.n_heads / 2;
   const int rows = m_hint > 0 ? m_hint : m_cap;
-  aa.splits = diff_attention_splits(rows, rows, nseq, aa.heads, dh, partial_bytes(ctx) / m_cap * rows, ctx->cus);
+  aa.tiles = diff_attention_tiles(rows, aa.heads, bf, ctx->cus);
+  aa.splits = aa.tiles ? 1 : diff_attention_splits(rows, rows, nseq, aa.heads, dh, partial_bytes(ctx) / m_cap * rows, ctx->cus);
   aa.partial = static_cast<float*>(ctx->h);
   aa.err_flag = ctx->err_flag;
 
@@ -1847,7 +1849,8 @@ CFDETR_API cfdetr_status cfdetr_diff_attention(cfdetr_ctx* ctx, const void* q, i
   a.eps = c.ln_eps;
   a.heads = c.n_heads / 2;
   const int dh = c.d_model / c.n_heads;
-  a.splits = diff_attention_splits(n_q, n_k, B, a.heads, dh, partial_bytes(ctx), ctx->cus);
+  a.tiles = diff_attention_tiles(n_q, a.heads, ctx->bf16, ctx->cus);
+  a.splits = a.tiles ? 1 : diff_attention_splits(n_q, n_k, B, a.heads, dh, partial_bytes(ctx), ctx->cus);
   a.partial = static_cast<float*>(ctx->h);
   a.err_flag = ctx->err_flag;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

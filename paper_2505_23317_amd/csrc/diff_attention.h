@@ -1,0 +1,240 @@
+// What the kernels of the differential attention share (diff_attention.hip, diff_tiles.hip).
+#pragma once
+#include <type_traits>
+
+#include "kernels.h"
+
+namespace cfdetr {
+
+namespace {
+
+constexpr int kThreads = 256;   // four wavefronts
+constexpr int kUnitKeys = 32;   // keys of one step of a wavefront
+
+__device__ __forceinline__ int swap_bits_2_3(int i) { return (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1); }
+
+// Where the frames of a batch lie: lane l of every wavefront holds the offsets of frames 2l and 2l + 1
+// (the merged run of the encoder has two sequences for each of up to 64 cameras).
+struct Frames {
+  int q[3], k[3];
+  bool bad;   // a negative length, or an end beyond the rows: the whole call is refused
+};
+__device__ __forceinline__ Frames frames_of(const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k, int B, int n_q, int n_k) {
+  const int l = 2 * (threadIdx.x & 63);
+  Frames f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    f.q[i] = cu_q[min(l + i, B)];
+    f.k[i] = cu_k[min(l + i, B)];
+    bad |= f.q[i] < 0 || f.k[i] < 0 || f.q[i] > n_q || f.k[i] > n_k || (i > 0 && (f.q[i] < f.q[i - 1] || f.k[i] < f.k[i - 1]));
+  }
+  f.bad = __any(bad || (l == 0 && (f.q[0] != 0 || f.k[0] != 0)));
+  return f;
+}
+// The frame that piece `id` belongs to, where a frame has pieces[0 or 1] of them (lane's two frames); `id` becomes
+// the piece's number within it.  -1: there are fewer.
+__device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int& id) {
+  const int lane = threadIdx.x & 63;
+  int upto = pieces[0] + pieces[1];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o);
+    if (lane >= o) upto += v;
+  }
+  const uint64_t in = __ballot(upto > id);
+  if (in == 0) return -1;
+  const int l = __ffsll((unsigned long long)in) - 1;
+  const int first = __builtin_amdgcn_readlane(pieces[0], l);
+  id -= __builtin_amdgcn_readlane(upto, l) - first - __builtin_amdgcn_readlane(pieces[1], l);
+  if (id < first) return 2 * l;
+  id -= first;
+  return 2 * l + 1;
+}
+__device__ __forceinline__ int of_frame(const int (&offsets)[3], int frame) {
+  const int even = __builtin_amdgcn_readlane(offsets[0], frame >> 1), odd = __builtin_amdgcn_readlane(offsets[1], frame >> 1);
+  return (frame & 1) ? odd : even;
+}
+__device__ __forceinline__ int behind_frame(const int (&offsets)[3], int frame) {
+  const int even = __builtin_amdgcn_readlane(offsets[1], frame >> 1), odd = __builtin_amdgcn_readlane(offsets[2], frame >> 1);
+  return (frame & 1) ? odd : even;
+}
+
+// ---- elements --------------------------------------------------------------------------
+// bf16: operands of 32x32x16 products, 8 elements a lane and step.  fp32: of 32x32x2 products, one.
+// In both, an operand row in LDS or memory is cut into chunks of 16 bytes and a lane of group g (lanes 32 g on)
+// has chunk 2c + g of chunk pair c.  S^T = K Q^T leaves a lane with 16 keys of one query.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<bf16_t> {
+  static constexpr int kChunk = 8;   // elements of 16 bytes
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ f32x16 dot(const uint4& k, const uint4& q, f32x16 acc) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&k), *reinterpret_cast<const bf16x8*>(&q), acc, 0, 0, 0);
+  }
+  // LDS row of a key, so that eight consecutive result registers of a lane are eight consecutive keys
+  static __device__ __forceinline__ int row_of_key(int key) { return swap_bits_2_3(key); }
+  // key of result register r of lane group g
+  static __device__ __forceinline__ int key_of(int r, int g) { return 16 * (r >> 3) + 8 * g + (r & 7); }
+};
+template <>
+struct Elem<float> {
+  static constexpr int kChunk = 4;
+  static __device__ __forceinline__ f32x16 dot(const uint4& k, const uint4& q, f32x16 acc) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.x), __uint_as_float(q.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.y), __uint_as_float(q.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.z), __uint_as_float(q.z), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k.w), __uint_as_float(q.w), acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ int row_of_key(int key) { return key; }
+  static __device__ __forceinline__ int key_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
+};
+
+// Order of a row's chunks in LDS.  Keys: 16 rows that are read together lie in all banks.  Values: blocks of 32
+// columns, moved so that the rows a product reads together lie in different banks.
+template <typename T, int ROWB>
+__device__ __forceinline__ int key_chunk(int row, int c) {
+  return ROWB == 128 ? c ^ ((row >> 1) & 7) : c ^ (row & 15);
+}
+template <typename T, int ROWB>
+__device__ __forceinline__ int value_block(int row, int b) {
+  if constexpr (std::is_same_v<T, float>) return b ^ ((row >> 2) & 1);
+  return ROWB == 128 ? b ^ ((row >> 1) & 1) : b ^ (row & 3);
+}
+
+// Sum of v over the lanes l and l ^ 32, and the larger of the two.
+__device__ __forceinline__ float half_sum(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float half_max(float v) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row16(T* to, const float (&x)[16]);
+template <>
+__device__ __forceinline__ void store_row16<bf16_t>(bf16_t* to, const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<uint4*>(to)[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
+                                                 pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
+}
+template <>
+__device__ __forceinline__ void store_row16<float>(float* to, const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(to)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+template <typename T>
+__device__ __forceinline__ void store_row8(T* to, const float (&x)[8]);
+template <>
+__device__ __forceinline__ void store_row8<bf16_t>(bf16_t* to, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+template <>
+__device__ __forceinline__ void store_row8<float>(float* to, const float (&x)[8]) {
+  reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// One unit of keys (in LDS, `left` of them keys of the frame) into the running maxima, sums and rows of a wavefront's 32
+// queries.
+template <typename T, int DH>
+__device__ __forceinline__ void online_unit(const unsigned char* sK, const unsigned char* sV, const uint4 (&qf)[2][DH * (int)sizeof(T) / 32],
+                                            int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][DH / 16]) {
+  constexpr int ROWB = 2 * DH * (int)sizeof(T), KS = ROWB / 64, MO = DH / 16;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  f32x16 s[2];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < KS; ++c)
+      s[m] = Elem<T>::dot(*reinterpret_cast<const uint4*>(sK + l32 * ROWB + key_chunk<T, ROWB>(l32, m * 2 * KS + 2 * c + g) * 16),
+                          qf[m][c], s[m]);
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[m][r] = Elem<T>::key_of(r, g) < left ? s[m][r] * scale2 : -INFINITY;
+      top = fmaxf(top, s[m][r]);
+    }
+    const float m_new = fmaxf(m_run[m], half_max(top));
+    const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m_run[m] - m_ref);
+    m_run[m] = m_new;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[m][r] = __builtin_amdgcn_exp2f(s[m][r] - m_ref);
+      sum += s[m][r];
+    }
+    l_run[m] = l_run[m] * alpha + sum;
+    if (__any(alpha != 1.0f)) {   // seldom behind the first units
+#pragma unroll
+      for (int i = 0; i < MO; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[m][i][r] *= alpha;
+    }
+  }
+  if constexpr (std::is_same_v<T, bf16_t>) {
+    // A rounding of the probabilities to bf16: half a step of 2^-8 each, independent between keys.
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 p[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        uint4 w = make_uint4(pack_bf16x2(s[m][8 * t], s[m][8 * t + 1]), pack_bf16x2(s[m][8 * t + 2], s[m][8 * t + 3]),
+                             pack_bf16x2(s[m][8 * t + 4], s[m][8 * t + 5]), pack_bf16x2(s[m][8 * t + 6], s[m][8 * t + 7]));
+        p[m] = *reinterpret_cast<bf16x8*>(&w);
+      }
+#pragma unroll
+      for (int i = 0; i < MO; ++i) {
+        // values come row by row; the transposing read gives a lane four keys of its column, a group of 16 lanes
+        // naming the pieces of four keys by 16 columns
+        union {
+          s16x4 half[2];
+          bf16x8 whole;
+        } v;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          const int key = 16 * t + 8 * g + 4 * hh + ((lane & 15) >> 2);
+          v.half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds4)(sV + key * ROWB + value_block<T, ROWB>(key, i) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8));
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.whole, p[m], acc[m][i], 0, 0, 0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = Elem<T>::key_of(r, g);
+#pragma unroll
+      for (int i = 0; i < MO; ++i) {
+        const float v = *reinterpret_cast<const float*>(sV + key * ROWB + value_block<T, ROWB>(key, i) * 128 + l32 * 4);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[m][r], acc[m][i], 0, 0, 0);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+// The kernel for many queries (diff_tiles.hip), bf16.
+hipError_t launch_diff_tiles(const DiffAttentionArgs& a, int d_head, hipStream_t s);
+
+}  // namespace cfdetr

@@ -459,11 +459,14 @@ struct DiffAttentionArgs {
   const float *lambda, *head_g;
   float scale2, eps;
   int heads;   // differential heads
+  bool tiles;  // diff_attention_tiles
   int splits;
   float* partial;
   int32_t* err_flag;
 };
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
+// Whether about n_q query rows go to the kernel of 128 queries a workgroup, and else into how many runs the keys are cut.
+bool diff_attention_tiles(int n_q, int heads, bool use_bf16, int cus);
 int diff_attention_splits(int n_q, int n_k, int B, int heads, int d_head, uint64_t partial_bytes, int cus);
 // list, kv_len: the keys of every frame whose mask byte is not 0, for launch_diff_attention.
 hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int n_k, int32_t* list, int32_t* kv_len, hipStream_t s);

@@ -74,6 +74,45 @@ def test_longer_frames(K, d, n):
     _run(K, d, n, n)
 
 
+# Frames of every length about a unit of 32 keys and a tile of 128 queries, often enough for the kernel of many queries (rows times
+# heads from 16,384 on, on 256 CUs), empty ones between them.
+EDGES = [0, 1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 0, 160, 255, 256, 257, 300, 513, 0]
+
+
+def _many(d):
+    n, heads = [], T.MODELS[d] // 2
+    while sum(n) * heads < 20_000:
+        n += EDGES
+    return n[:63] + [20_000 // heads - sum(n[:63])] if len(n) > 64 else n
+
+
+@pytest.mark.parametrize("norm", (True, False))
+@pytest.mark.parametrize("d", (64, 256, 384, 768, 1024))
+def test_many_queries(K, d, norm):
+    n = _many(d)
+    _run(K, d, n, n, norm=norm, scale=0.2 if norm else None)
+
+
+@pytest.mark.parametrize("d", (256, 384))
+def test_many_queries_over_other_rows(K, d):
+    n = _many(d)
+    _run(K, d, n, [(7 * m + 3) % 211 for m in n])
+
+
+@pytest.mark.parametrize("d,share", [(256, 0.5), (384, 0.1), (384, 0.95)])
+def test_many_queries_masked(K, d, share):
+    import torch
+    n = _many(d)
+    q, k, v = (x.clone() for x in _inputs(d, n, n, "bf16"))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(9)
+    mask = (torch.rand(sum(n), generator=g, device="cuda") >= share).to(torch.uint8)
+    mask[sum(n[:20]):sum(n[:21])] = 0
+    k[mask == 0], v[mask == 0] = math.nan, math.inf
+    out = _run(K, d, n, n, mask=mask, qkv=(q, k, v))
+    assert not out[sum(n[:20]):sum(n[:21])].any()
+
+
 def test_many_frames(K):
     """As many as a context takes, most of them short."""
     n = [(i * 37) % 91 for i in range(64)]
@@ -125,7 +164,7 @@ def test_masks_that_leave_everything_or_nothing(K):
     enc.close()
 
 
-@pytest.mark.parametrize("n", ([1, 63, 64, 65, 129, 200, 1000], [1500] * 2))
+@pytest.mark.parametrize("n", ([1, 63, 64, 65, 129, 200, 1000], [1500] * 2, [1, 63, 65, 129, 200, 1000] * 6))
 @pytest.mark.parametrize("level", (-400.0, -90.0, 90.0, 400.0))
 @pytest.mark.parametrize("d", (256, 384))
 def test_logits_far_from_zero(K, d, n, level):
@@ -184,6 +223,24 @@ def test_no_numbers_stay_in_their_frame(K):
     bad = ~torch.isfinite(out)
     assert bad[40:80, :64].all() and not bad[:40].any() and not bad[40:80, 64:].any()
     assert bad[80:, 70].all() and bad[80:].sum() == 200
+    enc.close()
+
+
+@pytest.mark.parametrize("d", (256, 384))
+def test_no_numbers_among_many_queries(K, d):
+    """A value that is no number reaches its column of the rows of its frame, the last key's too."""
+    import torch
+    n = [3000, 129, 3000, 97]
+    q, k, v = (x.clone() for x in _inputs(d, n, n, "bf16", std=0.3))
+    k[10, 3], v[3000 + 128, 70], v[6129 + 96, 5] = math.nan, math.inf, -math.inf
+    w = 2 * d // T.MODELS[d]
+    enc = T.encoder(d, sum(n), 4)
+    out = torch.empty(sum(n), d, device="cuda").bfloat16()
+    enc.diff_attention(q, k, v, T.offsets(n), T.offsets(n), torch.full((T.MODELS[d] // 2,), 0.0, device="cuda"), out)
+    bad = ~torch.isfinite(out)
+    assert bad[:3000, :w].all() and not bad[:3000, w:].any() and not bad[3129:6129].any()
+    assert (out[3000:3129, 70] == math.inf).all() and bad[3000:3129].sum() == 129
+    assert (out[6129:, 5] == -math.inf).all() and bad[6129:].sum() == 97
     enc.close()
 
 
