@@ -17,10 +17,11 @@ SOURCES = ["api.hip", "select.hip", "roi.hip", "rowwise.hip", "gemm.hip", "layer
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-kernarg-preload-count=16"]
-# Per-source extras.  The attention kernel reads every MFMA result back for the
+# Per-source extras.  The attention kernels read every MFMA result back for the
 # softmax, so its accumulators should live in ordinary VGPRs (no AGPR copies); the
 # GEMMs only read theirs in the epilogue and are faster with AGPR accumulators.
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "diff_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "diff_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 

@@ -73,7 +73,7 @@ struct Elem<bf16_t> {
   static __device__ __forceinline__ f32x16 dot(const uint4& k, const uint4& q, f32x16 acc) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&k), *reinterpret_cast<const bf16x8*>(&q), acc, 0, 0, 0);
   }
-  // LDS row of a key, so that eight consecutive result registers of a lane are eight consecutive keys
+  // LDS row of a key and its values, so that eight consecutive result registers of a lane are eight consecutive keys
   static __device__ __forceinline__ int row_of_key(int key) { return swap_bits_2_3(key); }
   // key of result register r of lane group g
   static __device__ __forceinline__ int key_of(int r, int g) { return 16 * (r >> 3) + 8 * g + (r & 7); }
@@ -147,28 +147,39 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// One unit of keys (in LDS, `left` of them keys of the frame) into the running maxima, sums and rows of a wavefront's 32
-// queries.
+// A unit of 32 keys with a running maximum, in three parts: the logits of a wavefront's 32 queries, their weights and
+// what those make of the sums so far, and the values under the weights.  Keys and values lie in LDS, in rows
+// of Elem::row_of_key; `left` of them are keys of the frame, and the values of the others are numbers.
 template <typename T, int DH>
-__device__ __forceinline__ void online_unit(const unsigned char* sK, const unsigned char* sV, const uint4 (&qf)[2][DH * (int)sizeof(T) / 32],
-                                            int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][DH / 16]) {
-  constexpr int ROWB = 2 * DH * (int)sizeof(T), KS = ROWB / 64, MO = DH / 16;
+__device__ __forceinline__ void unit_logits(const unsigned char* sK, const uint4 (&qf)[2][DH * (int)sizeof(T) / 32], f32x16 (&s)[2]) {
+  constexpr int ROWB = 2 * DH * (int)sizeof(T), KS = ROWB / 64;
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
-  f32x16 s[2];
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
+  for (int m = 0; m < 2; ++m)
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[m][r] = 0.f;
 #pragma unroll
-    for (int c = 0; c < KS; ++c)
+  for (int c = 0; c < KS; ++c)
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
       s[m] = Elem<T>::dot(*reinterpret_cast<const uint4*>(sK + l32 * ROWB + key_chunk<T, ROWB>(l32, m * 2 * KS + 2 * c + g) * 16),
                           qf[m][c], s[m]);
+}
+template <typename T, int MO>
+__device__ __forceinline__ void unit_weights(f32x16 (&s)[2], int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][MO]) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
     float top = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[m][r] = Elem<T>::key_of(r, g) < left ? s[m][r] * scale2 : -INFINITY;
-      top = fmaxf(top, s[m][r]);
+    for (int r = 0; r < 16; ++r) s[m][r] *= scale2;
+    if (left < kUnitKeys) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (Elem<T>::key_of(r, g) >= left) s[m][r] = -INFINITY;
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[m][r]);
     const float m_new = fmaxf(m_run[m], half_max(top));
     const float m_ref = m_new == -INFINITY ? 0.f : m_new;
     const float alpha = __builtin_amdgcn_exp2f(m_run[m] - m_ref);
@@ -187,8 +198,13 @@ __device__ __forceinline__ void online_unit(const unsigned char* sK, const unsig
         for (int r = 0; r < 16; ++r) acc[m][i][r] *= alpha;
     }
   }
+}
+template <typename T, int DH>
+__device__ __forceinline__ void unit_rows(const unsigned char* sV, const f32x16 (&s)[2], f32x16 (&acc)[2][DH / 16]) {
+  constexpr int ROWB = 2 * DH * (int)sizeof(T), MO = DH / 16;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   if constexpr (std::is_same_v<T, bf16_t>) {
-    // A rounding of the probabilities to bf16: half a step of 2^-8 each, independent between keys.
+    // A rounding of the weights to bf16: half a step of 2^-8 each, independent between keys.
     typedef __attribute__((ext_vector_type(4))) short s16x4;
     typedef __attribute__((address_space(3))) s16x4* lds4;
 #pragma unroll
@@ -210,9 +226,9 @@ __device__ __forceinline__ void online_unit(const unsigned char* sK, const unsig
         } v;
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-          const int key = 16 * t + 8 * g + 4 * hh + ((lane & 15) >> 2);
+          const int row = 16 * t + 8 * hh + 4 * g + ((lane & 15) >> 2);   // of keys 16 t + 8 g + 4 hh on
           v.half[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds4)(sV + key * ROWB + value_block<T, ROWB>(key, i) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8));
+              (lds4)(sV + row * ROWB + value_block<T, ROWB>(row, i) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8));
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.whole, p[m], acc[m][i], 0, 0, 0);
@@ -230,6 +246,23 @@ __device__ __forceinline__ void online_unit(const unsigned char* sK, const unsig
       }
     }
   }
+}
+
+// One 16-byte piece per lane from global memory straight into LDS (1 KB a wavefront at lds_addr, in lane order).  The
+// compiler does not count these loads: whoever reads them waits with vmcnt first.
+__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(sbase) : "memory");
+}
+__device__ __forceinline__ void dma16(const void* from, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(from) : "memory");
+}
+// Which chunk of 16 bytes lies at place `c` of an LDS row of keys, and of values (both orders are their own inverse).
+template <typename T, int ROWB>
+__device__ __forceinline__ int key_piece(int row, int c) { return key_chunk<T, ROWB>(row, c); }
+template <typename T, int ROWB>
+__device__ __forceinline__ int value_piece(int row, int c) {
+  constexpr int CPB = 2 * (int)sizeof(T);   // chunks of a block of 32 columns
+  return value_block<T, ROWB>(row, c / CPB) * CPB + c % CPB;
 }
 
 }  // namespace

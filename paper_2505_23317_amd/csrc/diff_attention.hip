@@ -15,21 +15,27 @@ namespace {
 constexpr int kTileQ = 32;      // queries of a workgroup (a lane each)
 
 // ---- few queries, or fp32 ----------------------------------------------------------------
-// A workgroup has 32 queries of one head and frame and one of `splits` runs of its keys; its four wavefronts take
+// A workgroup has 32 queries of one head and frame and one of `splits` runs of its keys.  Its four wavefronts take
 // units of 32 keys in turn, each with a running maximum and sum of both maps, through LDS of its own, so that
-// there is no barrier before the end.  There the four partial results are brought to one maximum and added up in LDS.
+// there is no barrier before the end: a unit's keys are asked for as soon as the logits of the unit before have been
+// taken, its values behind that unit's.  At the end the four partial results are brought to one maximum and
+// added up in LDS, one map after the other.
 // splits > 1: row, head and split leave their maxima, sums and unscaled rows in `partial`, which
 // diff_join_kernel adds up in a fixed order.
 template <typename T, int DH>
-__global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs a) {
-  constexpr int W = 2 * DH;                         // columns of both keys of a head, and of its values
-  constexpr int ROWB = W * (int)sizeof(T);          // bytes of such a row
-  constexpr int CPR = ROWB / 16;                    // chunks of it
+struct Few {
+  static constexpr int W = 2 * DH;                     // columns of both keys of a head, and of its values
+  static constexpr int ROWB = W * (int)sizeof(T);      // bytes of such a row
+  static constexpr int UNIT = kUnitKeys * ROWB;
+  static constexpr int WAVE = 2 * UNIT > 32 * W * 4 ? 2 * UNIT : 32 * W * 4;   // LDS of a wavefront: keys and values, then the rows of a map
+};
+template <typename T, int DH, bool LIST>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_kernel(DiffAttentionArgs a) {
+  constexpr int W = Few<T, DH>::W, ROWB = Few<T, DH>::ROWB, UNIT = Few<T, DH>::UNIT, WAVE = Few<T, DH>::WAVE;
+  constexpr int CPR = ROWB / 16;                    // chunks of a row
   constexpr int KS = CPR / 4;                       // chunk pairs of one map
   constexpr int MO = W / 32;                        // blocks of 32 output columns
-  constexpr int LI = kUnitKeys * CPR / 64;          // chunks of a unit's keys (and of its values) a lane
-  constexpr int UNIT = kUnitKeys * ROWB;
-  constexpr int WAVE = 2 * UNIT > 2 * 32 * W * 4 ? 2 * UNIT : 2 * 32 * W * 4;   // LDS of a wavefront: keys and values, then its two maps' rows
+  constexpr int NI = UNIT / 1024, RPI = 1024 / ROWB;   // loads of a unit's keys, rows of one
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   __shared__ float s_m[4][2][32], s_l[4][2][32];
 
@@ -53,9 +59,10 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
 
   const T* const kbase = static_cast<const T*>(a.k) + (size_t)k0 * a.k_ld + head * W;
   const T* const vbase = static_cast<const T*>(a.v) + (size_t)k0 * a.v_ld + head * W;
-  const int32_t* const list = a.key_list ? a.key_list + k0 : nullptr;
+  const int32_t* const list = LIST ? a.key_list + k0 : nullptr;
   unsigned char* const sK = smem + wave * WAVE;
   unsigned char* const sV = sK + UNIT;
+  const uint32_t ldsK = (uint32_t)(uintptr_t)sK, ldsV = ldsK + UNIT;
 
   uint4 qf[2][KS];
   {
@@ -66,17 +73,22 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
 #pragma unroll
       for (int c = 0; c < KS; ++c) qf[m][c] = *reinterpret_cast<const uint4*>(qrow + m * DH + (2 * c + g) * Elem<T>::kChunk);
   }
-  uint4 kr[LI], vr[LI];
-  auto fetch = [&](int u) {   // a unit's keys and values; past the last key zeros
+  // The rows of a unit: piece `lane` of load j lies in LDS row RPI j + lane / CPR.  Behind the last key they are the last
+  // key's again.
+  int at[NI];
+  auto rows_of = [&](int u) {
 #pragma unroll
-    for (int j = 0; j < LI; ++j) {
-      const int p = 64 * j + lane, key = p / CPR, c = p % CPR, at = u * kUnitKeys + key;
-      kr[j] = vr[j] = make_uint4(0, 0, 0, 0);
-      if (at < nk) {
-        const size_t row = list ? list[at] : at;
-        kr[j] = *reinterpret_cast<const uint4*>(kbase + row * a.k_ld + c * Elem<T>::kChunk);
-        vr[j] = *reinterpret_cast<const uint4*>(vbase + row * a.v_ld + c * Elem<T>::kChunk);
-      }
+    for (int j = 0; j < NI; ++j) {
+      at[j] = min(u * kUnitKeys + Elem<T>::row_of_key(RPI * j + lane / CPR), nk - 1);   // (row_of_key is its own inverse)
+      if constexpr (LIST) at[j] = list[at[j]];
+    }
+  };
+  auto load = [&](const T* base, int ld, bool values, uint32_t to) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int row = RPI * j + lane / CPR, c = lane % CPR;
+      const int piece = values ? value_piece<T, ROWB>(row, c) : key_piece<T, ROWB>(row, c);
+      dma16(base + (size_t)at[j] * ld + piece * Elem<T>::kChunk, to + j * 1024);
     }
   };
   f32x16 acc[2][MO];
@@ -89,23 +101,38 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
       for (int r = 0; r < 16; ++r) acc[m][i][r] = 0.f;
 
   int u = split * share + wave;
-  if (u < u_end) fetch(u);
+  if (u < u_end) {
+    rows_of(u);
+    load(kbase, a.k_ld, false, ldsK);
+    load(vbase, a.v_ld, true, ldsV);
+  }
 #pragma nounroll
   for (; u < u_end; u += 4) {
-    wave_fence();
-#pragma unroll
-    for (int j = 0; j < LI; ++j) {
-      const int p = 64 * j + lane, key = p / CPR, c = p % CPR, row = Elem<T>::row_of_key(key);
-      *reinterpret_cast<uint4*>(sK + row * ROWB + key_chunk<T, ROWB>(row, c) * 16) = kr[j];
-      constexpr int CPB = 32 * (int)sizeof(T) / 16;   // chunks of a block of 32 columns
-      *reinterpret_cast<uint4*>(sV + key * ROWB + (value_block<T, ROWB>(key, c / CPB) * CPB + c % CPB) * 16) = vr[j];
+    const bool more = u + 4 < u_end;
+    const int left = nk - u * kUnitKeys;
+    // (the keys; their values, asked for behind them, may still be on their way)
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
+    if (more) rows_of(u + 4);
+    f32x16 s[2];
+    unit_logits<T, DH>(sK, qf, s);
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    if (more) load(kbase, a.k_ld, false, ldsK);
+    unit_weights<T>(s, left, a.scale2, m_run, l_run, acc);
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    if (left < kUnitKeys) {
+      // weight 0 times what the last key's values are may be no number
+      for (int p = lane; p < (kUnitKeys - left) * CPR; p += 64)
+        *reinterpret_cast<uint4*>(sV + Elem<T>::row_of_key(left + p / CPR) * ROWB + p % CPR * 16) = make_uint4(0, 0, 0, 0);
+      wave_fence();
     }
-    if (u + 4 < u_end) fetch(u + 4);
-    wave_fence();
-    online_unit<T, DH>(sK, sV, qf, nk - u * kUnitKeys, a.scale2, m_run, l_run, acc);
+    unit_rows<T, DH>(sV, s, acc);
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    if (more) load(vbase, a.v_ld, true, ldsV);
   }
 
-  // The four wavefronts' results to one maximum, and into LDS: row of a query, its quads of columns moved by the query.
+  // The four wavefronts' results to one maximum, and map by map into LDS: row of a query, its quads of columns moved by the
+  // query.  Thread: query tid / 8, an eighth of its columns.
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     l_run[m] = half_sum(l_run[m]);
@@ -115,12 +142,15 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
     }
   }
   __syncthreads();
-  float top[2];
+  constexpr int CE = W / 8;
+  const int qi = tid >> 3, part = tid & 7;
+  const int q_local = tile * kTileQ + qi;
+  float o[2][CE], l_all[2], m_all[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    top[m] = fmaxf(fmaxf(s_m[0][m][l32], s_m[1][m][l32]), fmaxf(s_m[2][m][l32], s_m[3][m][l32]));
-    const float f = __builtin_amdgcn_exp2f(m_run[m] - (top[m] == -INFINITY ? 0.f : top[m]));
-    float* const rows = reinterpret_cast<float*>(sK) + m * 32 * W + l32 * W;
+    const float top = fmaxf(fmaxf(s_m[0][m][l32], s_m[1][m][l32]), fmaxf(s_m[2][m][l32], s_m[3][m][l32]));
+    const float f = __builtin_amdgcn_exp2f(m_run[m] - (top == -INFINITY ? 0.f : top));
+    float* const rows = reinterpret_cast<float*>(sK) + l32 * W;
 #pragma unroll
     for (int i = 0; i < MO; ++i)
 #pragma unroll
@@ -129,15 +159,7 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
         *reinterpret_cast<float4*>(rows + 4 * (quad ^ (l32 & (W / 4 - 1)))) =
             make_float4(acc[m][i][4 * rq] * f, acc[m][i][4 * rq + 1] * f, acc[m][i][4 * rq + 2] * f, acc[m][i][4 * rq + 3] * f);
       }
-  }
-  __syncthreads();
-  // thread: query tid / 8, an eighth of its columns
-  constexpr int CE = W / 8;
-  const int qi = tid >> 3, part = tid & 7;
-  const int q_local = tile * kTileQ + qi;
-  float o[2][CE], l_all[2], m_all[2];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
+    __syncthreads();
     m_all[m] = fmaxf(fmaxf(s_m[0][m][qi], s_m[1][m][qi]), fmaxf(s_m[2][m][qi], s_m[3][m][qi]));
     l_all[m] = 0.f;
 #pragma unroll
@@ -145,16 +167,17 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       l_all[m] += s_l[w][m][qi] * __builtin_amdgcn_exp2f(s_m[w][m][qi] - (m_all[m] == -INFINITY ? 0.f : m_all[m]));
-      const float* const rows = reinterpret_cast<const float*>(smem + w * WAVE) + m * 32 * W + qi * W;
+      const float* const from = reinterpret_cast<const float*>(smem + w * WAVE) + qi * W;
 #pragma unroll
       for (int e = 0; e < CE / 4; ++e) {
-        const float4 v = *reinterpret_cast<const float4*>(rows + 4 * ((part * (CE / 4) + e) ^ (qi & (W / 4 - 1))));
+        const float4 v = *reinterpret_cast<const float4*>(from + 4 * ((part * (CE / 4) + e) ^ (qi & (W / 4 - 1))));
         o[m][4 * e] += v.x;
         o[m][4 * e + 1] += v.y;
         o[m][4 * e + 2] += v.z;
         o[m][4 * e + 3] += v.w;
       }
     }
+    if (m == 0) __syncthreads();
   }
   if (a.splits > 1) {
     if (q_local < nq) {
@@ -190,31 +213,48 @@ __global__ __launch_bounds__(kThreads, 1) void diff_few_kernel(DiffAttentionArgs
   }
 }
 
-// The splits' results of a row and head, by one wavefront: lane's quad of columns of map lane / 32, in split order.
+// The splits' results of a row and head, by one workgroup: wavefront w adds up splits w, w + 4, .. in that order, lane l
+// a quad of columns of map l / 32, and the four sums are added in order.
 template <typename T, int DH>
 __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffAttentionArgs a) {
   constexpr int W = 2 * DH, Q = W / 4;   // quads of a map: 32 or 16 lanes of its 32
-  if (frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad) return;
+  constexpr int ROW = 2 * W + 4;
+  __shared__ float4 s_o[3][64];
+  __shared__ float s_l[3][64];
   const int lane = threadIdx.x & 63, map = lane >> 5, quad = lane & 31;
-  const int item = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = item / a.heads, head = item - row * a.heads;
-  if (row >= a.cu_q[a.B]) return;
-  const float* const from = a.partial + (size_t)item * a.splits * (2 * W + 4);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = blockIdx.x, row = item / a.heads, head = item - row * a.heads;
+  const float* const from = a.partial + (size_t)item * a.splits * ROW;
+  const bool bad = frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad;
+  if (bad || row >= a.cu_q[a.B]) return;
   float m = -INFINITY;
-  for (int s = lane & 31; s < a.splits; s += 32) m = fmaxf(m, from[(size_t)s * (2 * W + 4) + map]);
+  for (int s = quad; s < a.splits; s += 32) m = fmaxf(m, from[(size_t)s * ROW + map]);
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
   const float m_ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.splits; ++s) {
-    const float* const p = from + (size_t)s * (2 * W + 4);
+#pragma unroll 4
+  for (int s = wave; s < a.splits; s += 4) {
+    const float* const p = from + (size_t)s * ROW;
     const float f = __builtin_amdgcn_exp2f(p[map] - m_ref);
     l = fmaf(p[2 + map], f, l);
     if (quad < Q) {
       const float4 v = *reinterpret_cast<const float4*>(p + 4 + map * W + 4 * quad);
       o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
     }
+  }
+  if (wave > 0) {
+    s_o[wave - 1][lane] = o;
+    s_l[wave - 1][lane] = l;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) {
+    const float4 v = s_o[w][lane];
+    o = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+    l += s_l[w][lane];
   }
   const float i = l != 0.f ? (map ? -a.lambda[head] : 1.0f) / l : 0.f;
   o = i != 0.f ? make_float4(o.x * i, o.y * i, o.z * i, o.w * i) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -286,18 +326,22 @@ __global__ __launch_bounds__(kThreads) void key_list_kernel(const uint8_t* __res
   if (end == nk && wave == 3 && lane == 0) kv_len[f] = at;
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool LIST>
 hipError_t few(const DiffAttentionArgs& a, hipStream_t s) {
-  constexpr int W = 2 * DH, UNIT = kUnitKeys * W * (int)sizeof(T);
-  constexpr int WAVE = 2 * UNIT > 2 * 32 * W * 4 ? 2 * UNIT : 2 * 32 * W * 4;
+  constexpr int LDS = 4 * Few<T, DH>::WAVE;
   static DeviceOnce once;
-  if (hipError_t e = allow_lds(diff_few_kernel<T, DH>, 4 * WAVE, &once); e != hipSuccess) return e;
-  const int64_t grid = ((int64_t)a.n_q / kTileQ + a.B) * a.heads * a.splits;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((diff_few_kernel<T, DH>), dim3((unsigned)grid), dim3(kThreads), 4 * WAVE, s, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((diff_join_kernel<T, DH>), dim3((unsigned)(((int64_t)a.n_q * a.heads + 3) / 4)), dim3(kThreads), 0, s, a);
+  if (hipError_t e = allow_lds(diff_few_kernel<T, DH, LIST>, LDS, &once); e != hipSuccess) return e;
+  const int64_t grid = ((int64_t)a.n_q / kTileQ + a.B) * a.heads * a.splits, rows = (int64_t)a.n_q * a.heads;
+  if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((diff_few_kernel<T, DH, LIST>), dim3((unsigned)grid), dim3(kThreads), LDS, s, a);
+  if (a.splits > 1) hipLaunchKernelGGL((diff_join_kernel<T, DH>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t few(const DiffAttentionArgs& a, int d_head, hipStream_t s) {
+  if (d_head == 64) return a.key_list ? few<T, 64, true>(a, s) : few<T, 64, false>(a, s);
+  if (d_head == 32) return a.key_list ? few<T, 32, true>(a, s) : few<T, 32, false>(a, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -319,9 +363,7 @@ bool diff_attention_tiles(int n_q, int heads, bool use_bf16, int cus) { return u
 
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s) {
   if (use_bf16 && a.tiles) return launch_diff_tiles(a, d_head, s);
-  if (d_head == 64) return use_bf16 ? few<bf16_t, 64>(a, s) : few<float, 64>(a, s);
-  if (d_head == 32) return use_bf16 ? few<bf16_t, 32>(a, s) : few<float, 32>(a, s);
-  return hipErrorInvalidValue;
+  return use_bf16 ? few<bf16_t>(a, d_head, s) : few<float>(a, d_head, s);
 }
 
 }  // namespace cfdetr

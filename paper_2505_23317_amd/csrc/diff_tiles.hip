@@ -102,22 +102,16 @@ __device__ __attribute__((noinline)) void redo_rows(const bf16_t* qrow, const bf
         vv = *reinterpret_cast<const uint4*>(vbase + from * v_ld + c * 8);
       }
       *reinterpret_cast<uint4*>(sK + row * ROWB + key_chunk<bf16_t, ROWB>(row, c) * 16) = kk;
-      *reinterpret_cast<uint4*>(sV + key * ROWB + (value_block<bf16_t, ROWB>(key, c / 4) * 4 + c % 4) * 16) = vv;
+      *reinterpret_cast<uint4*>(sV + row * ROWB + value_piece<bf16_t, ROWB>(row, c) * 16) = vv;
     }
     __syncthreads();
-    online_unit<bf16_t, DH>(sK, sV, qf, nk - k0, scale2, m_run, l_run, acc);
+    f32x16 s[2];
+    unit_logits<bf16_t, DH>(sK, qf, s);
+    unit_weights<bf16_t>(s, nk - k0, scale2, m_run, l_run, acc);
+    unit_rows<bf16_t, DH>(sV, s, acc);
   }
   const float l[2] = {half_sum(l_run[0]), half_sum(l_run[1])};
   finish_rows<DH>(acc, l, lambda, head_g, eps, orow, again);
-}
-
-// One 16-byte piece per lane from global memory straight into LDS (1 KB a wavefront at lds_addr, in lane order).  The
-// compiler does not count these loads: the stages wait with vmcnt themselves.
-__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(sbase) : "memory");
-}
-__device__ __forceinline__ void dma16(const void* from, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(from) : "memory");
 }
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -213,17 +207,16 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   // Loads: piece `lane` of instruction j of this wavefront lies in LDS row (wave NI + j) RPI + lane / CPR; which key and
   // chunk that is, is the order of the rows and chunks in LDS.
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-  int k_key[NI], v_key[NI];
+  int key[NI];
   uint32_t k_col[NI], v_col[NI];
 #pragma unroll
   for (int j = 0; j < NI; ++j) {
     const int rho = (wave * NI + j) * RPI + lane / CPR, c = lane % CPR;
-    k_key[j] = swap_bits_2_3(rho);
-    v_key[j] = rho;
-    k_col[j] = key_chunk<bf16_t, ROWB>(rho, c) * 16;
-    v_col[j] = (value_block<bf16_t, ROWB>(rho, c / 4) * 4 + c % 4) * 16;
+    key[j] = swap_bits_2_3(rho);
+    k_col[j] = key_piece<bf16_t, ROWB>(rho, c) * 16;
+    v_col[j] = value_piece<bf16_t, ROWB>(rho, c) * 16;
   }
-  auto load = [&](const bf16_t* base, int ld, const int(&key)[NI], const uint32_t(&col)[NI], int u, uint32_t to) {
+  auto load = [&](const bf16_t* base, int ld, const uint32_t(&col)[NI], int u, uint32_t to) {
     to += wave * (NI * 1024);
     if constexpr (LIST) {
 #pragma unroll
@@ -245,12 +238,12 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   };
   auto slot = [](int u, int slots) { return (uint32_t)(u % slots) * UNIT; };
   constexpr uint32_t VALUES = kKeySlots * UNIT;
-  auto load_k = [&](int u, uint32_t at) { load(kbase, a.k_ld, k_key, k_col, u, lds0 + at); };
-  auto load_v = [&](int u, uint32_t at) { load(vbase, a.v_ld, v_key, v_col, u, lds0 + VALUES + at); };
+  auto load_k = [&](int u, uint32_t at) { load(kbase, a.k_ld, k_col, u, lds0 + at); };
+  auto load_v = [&](int u, uint32_t at) { load(vbase, a.v_ld, v_col, u, lds0 + VALUES + at); };
 
   // Operands: row l32 of the keys, chunk 2 ks + g of a map; for the values the transposing read's pieces.
   const uint32_t k_at = l32 * ROWB + key_chunk<bf16_t, ROWB>(l32, g) * 16;
-  const int v_row = 8 * g + ((lane & 15) >> 2);
+  const int v_row = 4 * g + ((lane & 15) >> 2);   // of keys 8 g on; those of 8 g + 4 on are 8 rows behind
   const uint32_t v_at = VALUES + v_row * ROWB + value_block<bf16_t, ROWB>(v_row, 0) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   auto read_k = [&](uint32_t at, int kk) {   // operand kk = 2 ks + map (chunks and blocks are moved by bits: an exclusive or)
     return *reinterpret_cast<const bf16x8*>(smem + ((at + k_at) ^ (uint32_t)(((kk & 1) * 2 * KS + 2 * (kk >> 1)) * 16)));
@@ -262,7 +255,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
     } v;
     const uint32_t from = ((at + v_at) ^ (uint32_t)((p >> 1) * 64)) + (p & 1) * 16 * ROWB;
     v.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(smem + from));
-    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(smem + from + 4 * ROWB));
+    v.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(smem + from + 8 * ROWB));
     return v.whole;
   };
 
@@ -379,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
     mask(s);
     const uint32_t at = VALUES + slot(n - 1, kValueSlots);
     for (int p = tid; p < (kUnitKeys - ragged) * CPR; p += kThreads)
-      *reinterpret_cast<uint4*>(smem + at + ragged * ROWB + p * 16) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(smem + at + swap_bits_2_3(ragged + p / CPR) * ROWB + p % CPR * 16) = make_uint4(0, 0, 0, 0);
     __syncthreads();
   };
   auto final_pv = [&](bf16x8(&p)[2][2]) {
