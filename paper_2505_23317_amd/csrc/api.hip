@@ -451,8 +451,7 @@ cfdetr_status run_differential(cfdetr_ctx* ctx, int nseq, const RunShape& shape,
   aa.eps = c.ln_eps;
   aa.heads = c.n_heads / 2;
   const int rows = m_hint > 0 ? m_hint : m_cap;
-  aa.tiles = diff_attention_tiles(rows, aa.heads, bf, ctx->cus);
-  aa.splits = aa.tiles ? 1 : diff_attention_splits(rows, rows, nseq, aa.heads, dh, partial_bytes(ctx) / m_cap * rows, ctx->cus);
+  plan_diff_attention(aa, rows, rows, dh, bf, partial_bytes(ctx), ctx->cus);
   aa.partial = static_cast<float*>(ctx->h);
   aa.err_flag = ctx->err_flag;
 
@@ -1849,8 +1848,7 @@ CFDETR_API cfdetr_status cfdetr_diff_attention(cfdetr_ctx* ctx, const void* q, i
   a.eps = c.ln_eps;
   a.heads = c.n_heads / 2;
   const int dh = c.d_model / c.n_heads;
-  a.tiles = diff_attention_tiles(n_q, a.heads, ctx->bf16, ctx->cus);
-  a.splits = a.tiles ? 1 : diff_attention_splits(n_q, n_k, B, a.heads, dh, partial_bytes(ctx), ctx->cus);
+  plan_diff_attention(a, n_q, n_k, dh, ctx->bf16, partial_bytes(ctx), ctx->cus);
   a.partial = static_cast<float*>(ctx->h);
   a.err_flag = ctx->err_flag;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

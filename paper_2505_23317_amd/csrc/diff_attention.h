@@ -36,12 +36,16 @@ __device__ __forceinline__ Frames frames_of(const int32_t* __restrict__ cu_q, co
 // the piece's number within it.  -1: there are fewer.
 __device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int& id) {
   const int lane = threadIdx.x & 63;
+  // inclusive sum over the lanes, inside the vector unit: within rows of 16, then row 0 into 1 and 2 into 3, then 1 into 2 and 3
   int upto = pieces[0] + pieces[1];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(upto, o);
-    if (lane >= o) upto += v;
-  }
+  auto from = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, upto, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+  const auto all = std::integral_constant<int, 0xF>{};
+  upto += from(std::integral_constant<int, 0x111>{}, all);   // row_shr:1, 2, 4, 8
+  upto += from(std::integral_constant<int, 0x112>{}, all);
+  upto += from(std::integral_constant<int, 0x114>{}, all);
+  upto += from(std::integral_constant<int, 0x118>{}, all);
+  upto += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
+  upto += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
   const uint64_t in = __ballot(upto > id);
   if (in == 0) return -1;
   const int l = __ffsll((unsigned long long)in) - 1;
@@ -115,30 +119,22 @@ __device__ __forceinline__ float half_max(float v) {
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
-template <typename T>
-__device__ __forceinline__ void store_row16(T* to, const float (&x)[16]);
-template <>
-__device__ __forceinline__ void store_row16<bf16_t>(bf16_t* to, const float (&x)[16]) {
+template <typename T, int N>
+__device__ __forceinline__ void store_columns(T* to, const float (&x)[N]) {
+  static_assert(N % 4 == 0, "whole quads");
+  if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    reinterpret_cast<uint4*>(to)[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
-                                                 pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
-}
-template <>
-__device__ __forceinline__ void store_row16<float>(float* to, const float (&x)[16]) {
+    for (int i = 0; i < N / 4; ++i) reinterpret_cast<float4*>(to)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+  } else if constexpr (N % 8 == 0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) reinterpret_cast<float4*>(to)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-}
-template <typename T>
-__device__ __forceinline__ void store_row8(T* to, const float (&x)[8]);
-template <>
-__device__ __forceinline__ void store_row8<bf16_t>(bf16_t* to, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-}
-template <>
-__device__ __forceinline__ void store_row8<float>(float* to, const float (&x)[8]) {
-  reinterpret_cast<float4*>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    for (int i = 0; i < N / 8; ++i)
+      reinterpret_cast<uint4*>(to)[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
+                                                   pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      reinterpret_cast<uint2*>(to)[i] = make_uint2(pack_bf16x2(x[4 * i], x[4 * i + 1]), pack_bf16x2(x[4 * i + 2], x[4 * i + 3]));
+  }
 }
 
 __device__ __forceinline__ void wave_fence() {
@@ -165,38 +161,44 @@ __device__ __forceinline__ void unit_logits(const unsigned char* sK, const uint4
       s[m] = Elem<T>::dot(*reinterpret_cast<const uint4*>(sK + l32 * ROWB + key_chunk<T, ROWB>(l32, m * 2 * KS + 2 * c + g) * 16),
                           qf[m][c], s[m]);
 }
+// The reference of the weights follows the largest logit only once that is kSlack ahead (2^kSlack times the
+// others): a quotient is the same for any reference, and with 32 queries in a wavefront some largest logit moves in almost every
+// unit, which costs two operations for every sum (attention of 300 queries a frame, 1600 to 6400 tokens: 33 -> XX us).
+constexpr float kSlack = 16.f;
 template <typename T, int MO>
 __device__ __forceinline__ void unit_weights(f32x16 (&s)[2], int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][MO]) {
   const int g = (threadIdx.x & 63) >> 5;
+  if (left < kUnitKeys) {
 #pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[m][r] *= scale2;
-    if (left < kUnitKeys) {
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (Elem<T>::key_of(r, g) >= left) s[m][r] = -INFINITY;
-    }
+  }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[m][r]);
-    const float m_new = fmaxf(m_run[m], half_max(top));
-    const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(m_run[m] - m_ref);
-    m_run[m] = m_new;
-    float sum = 0.f;
+  for (int m = 0; m < 2; ++m) {
+    float top = s[m][0];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[m][r] = __builtin_amdgcn_exp2f(s[m][r] - m_ref);
-      sum += s[m][r];
-    }
-    l_run[m] = l_run[m] * alpha + sum;
-    if (__any(alpha != 1.0f)) {   // seldom behind the first units
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[m][r]);
+    top = half_max(top) * scale2;
+    if (__any(top > m_run[m] + kSlack)) {
+      const float m_new = fmaxf(m_run[m], top);
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[m] - m_new);
+      m_run[m] = m_new;
+      l_run[m] *= alpha;
 #pragma unroll
       for (int i = 0; i < MO; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[m][i][r] *= alpha;
     }
+    const float m_ref = m_run[m] == -INFINITY ? 0.f : m_run[m];   // (every logit of a query may be -infinity so far)
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[m][r] = __builtin_amdgcn_exp2f(fmaf(s[m][r], scale2, -m_ref));
+      sum += s[m][r];
+    }
+    l_run[m] += sum;
   }
 }
 template <typename T, int DH>
@@ -251,10 +253,10 @@ __device__ __forceinline__ void unit_rows(const unsigned char* sV, const f32x16 
 // One 16-byte piece per lane from global memory straight into LDS (1 KB a wavefront at lds_addr, in lane order).  The
 // compiler does not count these loads: whoever reads them waits with vmcnt first.
 __device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voff), "s"(sbase) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(sbase) : "memory");
 }
 __device__ __forceinline__ void dma16(const void* from, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(from) : "memory");
 }
 // Which chunk of 16 bytes lies at place `c` of an LDS row of keys, and of values (both orders are their own inverse).
 template <typename T, int ROWB>

@@ -13,6 +13,7 @@ namespace cfdetr {
 namespace {
 
 constexpr int kTileQ = 32;      // queries of a workgroup (a lane each)
+constexpr int kMostSplits = 128;
 
 // ---- few queries, or fp32 ----------------------------------------------------------------
 // A workgroup has 32 queries of one head and frame and one of `splits` runs of its keys.  Its four wavefronts take
@@ -29,15 +30,15 @@ struct Few {
   static constexpr int UNIT = kUnitKeys * ROWB;
   static constexpr int WAVE = 2 * UNIT > 32 * W * 4 ? 2 * UNIT : 32 * W * 4;   // LDS of a wavefront: keys and values, then the rows of a map
 };
-template <typename T, int DH, bool LIST>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_kernel(DiffAttentionArgs a) {
+template <typename T, int DH, bool LIST, int NW>
+__global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kernel(DiffAttentionArgs a) {
   constexpr int W = Few<T, DH>::W, ROWB = Few<T, DH>::ROWB, UNIT = Few<T, DH>::UNIT, WAVE = Few<T, DH>::WAVE;
   constexpr int CPR = ROWB / 16;                    // chunks of a row
   constexpr int KS = CPR / 4;                       // chunk pairs of one map
   constexpr int MO = W / 32;                        // blocks of 32 output columns
   constexpr int NI = UNIT / 1024, RPI = 1024 / ROWB;   // loads of a unit's keys, rows of one
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ float s_m[4][2][32], s_l[4][2][32];
+  __shared__ float s_m[NW][2][32], s_l[NW][2][32];
 
   const Frames fr = frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k);
   if (fr.bad) {
@@ -46,8 +47,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
   }
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.heads;
-  int tile = blockIdx.x / a.splits / a.heads;
+  // (the heads of a run of keys next to each other: they are columns of the same rows)
+  const int head = blockIdx.x % a.heads, split = blockIdx.x / a.heads % a.splits;
+  int tile = blockIdx.x / a.heads / a.splits;
   const int tiles[2] = {(fr.q[1] - fr.q[0] + kTileQ - 1) / kTileQ, (fr.q[2] - fr.q[1] + kTileQ - 1) / kTileQ};
   const int frame = frame_of_piece(tiles, tile);
   if (frame < 0) return;
@@ -73,24 +75,34 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
 #pragma unroll
       for (int c = 0; c < KS; ++c) qf[m][c] = *reinterpret_cast<const uint4*>(qrow + m * DH + (2 * c + g) * Elem<T>::kChunk);
   }
-  // The rows of a unit: piece `lane` of load j lies in LDS row RPI j + lane / CPR.  Behind the last key they are the last
-  // key's again.
-  int at[NI];
-  auto rows_of = [&](int u) {
+  // A unit's loads: piece `lane` of load j lies in LDS row RPI j + lane / CPR.  The key of that row is key_at(RPI j) + key_at(lane / CPR)
+  // (row_of_key moves bits and is its own inverse), so that a full unit of consecutive keys needs an offset a
+  // lane and its places in the row.  Rows behind the last key are the last key's again.  With a list lane l has the row of key l mod
+  // 32, asked for two units ahead, and the others fetch it from there.
+  auto key_at = [](int row) { return Elem<T>::row_of_key(row); };
+  const int within = key_at(lane / CPR), place = lane % CPR;
+  int listed = 0;
+  auto ask = [&](int u) {
+    if constexpr (LIST) listed = list[min(u * kUnitKeys + l32, nk - 1)];
+  };
+  auto load = [&](const T* base, int ld, auto values, int u, int rows, uint32_t to) {
+    const int last = nk - 1 - u * kUnitKeys;
+    const T* const from = base + (size_t)(u * kUnitKeys) * ld;
+    const uint32_t step = (uint32_t)ld * (uint32_t)sizeof(T);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      at[j] = min(u * kUnitKeys + Elem<T>::row_of_key(RPI * j + lane / CPR), nk - 1);   // (row_of_key is its own inverse)
-      if constexpr (LIST) at[j] = list[at[j]];
+      const int row = RPI * j + lane / CPR;
+      const uint32_t col = (uint32_t)(decltype(values)::value ? value_piece<T, ROWB>(row, place) : key_piece<T, ROWB>(row, place)) * 16;
+      if constexpr (LIST)
+        dma16(reinterpret_cast<const char*>(base) + (size_t)__shfl(rows, key_at(RPI * j) + within) * step + col, to + j * 1024);
+      else if (last >= kUnitKeys - 1)
+        dma16(from + (size_t)key_at(RPI * j) * ld, within * step + col, to + j * 1024);
+      else
+        dma16(from, (uint32_t)min(key_at(RPI * j) + within, last) * step + col, to + j * 1024);
     }
   };
-  auto load = [&](const T* base, int ld, bool values, uint32_t to) {
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int row = RPI * j + lane / CPR, c = lane % CPR;
-      const int piece = values ? value_piece<T, ROWB>(row, c) : key_piece<T, ROWB>(row, c);
-      dma16(base + (size_t)at[j] * ld + piece * Elem<T>::kChunk, to + j * 1024);
-    }
-  };
+  const auto of_keys = std::integral_constant<bool, false>{};
+  const auto of_values = std::integral_constant<bool, true>{};
   f32x16 acc[2][MO];
   float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
 #pragma unroll
@@ -102,21 +114,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
 
   int u = split * share + wave;
   if (u < u_end) {
-    rows_of(u);
-    load(kbase, a.k_ld, false, ldsK);
-    load(vbase, a.v_ld, true, ldsV);
+    ask(u);
+    load(kbase, a.k_ld, of_keys, u, listed, ldsK);
+    load(vbase, a.v_ld, of_values, u, listed, ldsV);
+    if (u + NW < u_end) ask(u + NW);
   }
 #pragma nounroll
-  for (; u < u_end; u += 4) {
-    const bool more = u + 4 < u_end;
-    const int left = nk - u * kUnitKeys;
+  for (; u < u_end; u += NW) {
+    const bool more = u + NW < u_end;
+    const int left = nk - u * kUnitKeys, rows = listed;
     // (the keys; their values, asked for behind them, may still be on their way)
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
-    if (more) rows_of(u + 4);
     f32x16 s[2];
     unit_logits<T, DH>(sK, qf, s);
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-    if (more) load(kbase, a.k_ld, false, ldsK);
+    if (more) load(kbase, a.k_ld, of_keys, u + NW, rows, ldsK);
     unit_weights<T>(s, left, a.scale2, m_run, l_run, acc);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
@@ -128,11 +140,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
     }
     unit_rows<T, DH>(sV, s, acc);
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-    if (more) load(vbase, a.v_ld, true, ldsV);
+    if (more) load(vbase, a.v_ld, of_values, u + NW, rows, ldsV);
+    if (u + 2 * NW < u_end) ask(u + 2 * NW);
   }
 
-  // The four wavefronts' results to one maximum, and map by map into LDS: row of a query, its quads of columns moved by the
-  // query.  Thread: query tid / 8, an eighth of its columns.
+  // The wavefronts' results to one maximum, and map by map into LDS: row of a query, its quads of columns moved by the
+  // query.  Thread: query tid / (2 NW), one part of its columns.
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     l_run[m] = half_sum(l_run[m]);
@@ -142,13 +155,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
     }
   }
   __syncthreads();
-  constexpr int CE = W / 8;
-  const int qi = tid >> 3, part = tid & 7;
+  constexpr int PARTS = 2 * NW, CE = W / PARTS;
+  const int qi = tid / PARTS, part = tid % PARTS;
   const int q_local = tile * kTileQ + qi;
+  auto highest = [&](int m, int q) {
+    float top = s_m[0][m][q];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][m][q]);
+    return top;
+  };
   float o[2][CE], l_all[2], m_all[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
-    const float top = fmaxf(fmaxf(s_m[0][m][l32], s_m[1][m][l32]), fmaxf(s_m[2][m][l32], s_m[3][m][l32]));
+    const float top = highest(m, l32);
     const float f = __builtin_amdgcn_exp2f(m_run[m] - (top == -INFINITY ? 0.f : top));
     float* const rows = reinterpret_cast<float*>(sK) + l32 * W;
 #pragma unroll
@@ -160,12 +179,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
             make_float4(acc[m][i][4 * rq] * f, acc[m][i][4 * rq + 1] * f, acc[m][i][4 * rq + 2] * f, acc[m][i][4 * rq + 3] * f);
       }
     __syncthreads();
-    m_all[m] = fmaxf(fmaxf(s_m[0][m][qi], s_m[1][m][qi]), fmaxf(s_m[2][m][qi], s_m[3][m][qi]));
+    m_all[m] = highest(m, qi);
     l_all[m] = 0.f;
 #pragma unroll
     for (int e = 0; e < CE; ++e) o[m][e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < NW; ++w) {
       l_all[m] += s_l[w][m][qi] * __builtin_amdgcn_exp2f(s_m[w][m][qi] - (m_all[m] == -INFINITY ? 0.f : m_all[m]));
       const float* const from = reinterpret_cast<const float*>(smem + w * WAVE) + qi * W;
 #pragma unroll
@@ -201,41 +220,45 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_few_ker
   }
   if (a.head_g) {
 #pragma unroll
-    for (int s = 1; s < 8; s <<= 1) sq += __shfl_xor(sq, s);
+    for (int s = 1; s < PARTS; s <<= 1) sq += __shfl_xor(sq, s);
     const float r = rsqrtf(sq * (1.0f / W) + a.eps);
 #pragma unroll
     for (int e = 0; e < CE; ++e) x[e] *= r * a.head_g[part * CE + e];
   }
   if (q_local < nq) {
     T* const to = static_cast<T*>(a.out) + (size_t)(q0 + q_local) * a.out_ld + head * W + part * CE;
-    if constexpr (CE == 16) store_row16<T>(to, x);
-    else store_row8<T>(to, x);
+    store_columns<T, CE>(to, x);
   }
 }
 
-// The splits' results of a row and head, by one workgroup: wavefront w adds up splits w, w + 4, .. in that order, lane l
-// a quad of columns of map l / 32, and the four sums are added in order.
-template <typename T, int DH>
-__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffAttentionArgs a) {
+// The splits' results of a row and head, by one workgroup: wavefront w adds up splits w, w + NW, .. in that order, lane l
+// a quad of columns of map l / 32, and the wavefronts' sums are added in order.
+template <typename T, int DH, int NW>
+__global__ __launch_bounds__(64 * NW) void diff_join_kernel(DiffAttentionArgs a) {
   constexpr int W = 2 * DH, Q = W / 4;   // quads of a map: 32 or 16 lanes of its 32
   constexpr int ROW = 2 * W + 4;
-  __shared__ float4 s_o[3][64];
-  __shared__ float s_l[3][64];
+  constexpr int STEPS = kMostSplits / 32;
+  __shared__ float4 s_o[NW][64];
+  __shared__ float s_l[NW][64];
   const int lane = threadIdx.x & 63, map = lane >> 5, quad = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int item = blockIdx.x, row = item / a.heads, head = item - row * a.heads;
   const float* const from = a.partial + (size_t)item * a.splits * ROW;
-  const bool bad = frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad;
-  if (bad || row >= a.cu_q[a.B]) return;
+  // (what is read here of a row behind the last frame, or after bad offsets, is not used)
   float m = -INFINITY;
-  for (int s = quad; s < a.splits; s += 32) m = fmaxf(m, from[(size_t)s * ROW + map]);
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int s = quad + 32 * i;
+    if (s < a.splits) m = fmaxf(m, from[(size_t)s * ROW + map]);
+  }
+  if (frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad || row >= a.cu_q[a.B]) return;
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
   const float m_ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int s = wave; s < a.splits; s += 4) {
+#pragma unroll 8
+  for (int s = wave; s < a.splits; s += NW) {
     const float* const p = from + (size_t)s * ROW;
     const float f = __builtin_amdgcn_exp2f(p[map] - m_ref);
     l = fmaf(p[2 + map], f, l);
@@ -244,14 +267,12 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffAttentionArgs a
       o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
     }
   }
-  if (wave > 0) {
-    s_o[wave - 1][lane] = o;
-    s_l[wave - 1][lane] = l;
-  }
+  s_o[wave][lane] = o;
+  s_l[wave][lane] = l;
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
-  for (int w = 0; w < 3; ++w) {
+  for (int w = 1; w < NW; ++w) {
     const float4 v = s_o[w][lane];
     o = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
     l += s_l[w][lane];
@@ -271,10 +292,8 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffAttentionArgs a
   }
   if (map == 0 && quad < Q) {
     T* const to = static_cast<T*>(a.out) + (size_t)row * a.out_ld + head * W + 4 * quad;
-    if constexpr (std::is_same_v<T, float>)
-      *reinterpret_cast<float4*>(to) = o;
-    else
-      *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+    const float x[4] = {o.x, o.y, o.z, o.w};
+    store_columns<T, 4>(to, x);
   }
 }
 
@@ -326,21 +345,31 @@ __global__ __launch_bounds__(kThreads) void key_list_kernel(const uint8_t* __res
   if (end == nk && wave == 3 && lane == 0) kv_len[f] = at;
 }
 
-template <typename T, int DH, bool LIST>
+template <typename T, int DH, bool LIST, int NW>
 hipError_t few(const DiffAttentionArgs& a, hipStream_t s) {
-  constexpr int LDS = 4 * Few<T, DH>::WAVE;
+  constexpr int LDS = NW * Few<T, DH>::WAVE;
   static DeviceOnce once;
-  if (hipError_t e = allow_lds(diff_few_kernel<T, DH, LIST>, LDS, &once); e != hipSuccess) return e;
+  if (hipError_t e = allow_lds(diff_few_kernel<T, DH, LIST, NW>, LDS, &once); e != hipSuccess) return e;
   const int64_t grid = ((int64_t)a.n_q / kTileQ + a.B) * a.heads * a.splits, rows = (int64_t)a.n_q * a.heads;
   if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((diff_few_kernel<T, DH, LIST>), dim3((unsigned)grid), dim3(kThreads), LDS, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL((diff_join_kernel<T, DH>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((diff_few_kernel<T, DH, LIST, NW>), dim3((unsigned)grid), dim3(64 * NW), LDS, s, a);
+  if (a.splits > 16)
+    hipLaunchKernelGGL((diff_join_kernel<T, DH, 16>), dim3((unsigned)rows), dim3(1024), 0, s, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL((diff_join_kernel<T, DH, 2>), dim3((unsigned)rows), dim3(128), 0, s, a);
   return hipGetLastError();
+}
+template <typename T, int DH>
+hipError_t few(const DiffAttentionArgs& a, hipStream_t s) {
+  // fp32 has LDS for four wavefronts
+  if constexpr (sizeof(T) == 2)
+    if (a.wide) return a.key_list ? few<T, DH, true, 8>(a, s) : few<T, DH, false, 8>(a, s);
+  return a.key_list ? few<T, DH, true, 4>(a, s) : few<T, DH, false, 4>(a, s);
 }
 template <typename T>
 hipError_t few(const DiffAttentionArgs& a, int d_head, hipStream_t s) {
-  if (d_head == 64) return a.key_list ? few<T, 64, true>(a, s) : few<T, 64, false>(a, s);
-  if (d_head == 32) return a.key_list ? few<T, 32, true>(a, s) : few<T, 32, false>(a, s);
+  if (d_head == 64) return few<T, 64>(a, s);
+  if (d_head == 32) return few<T, 32>(a, s);
   return hipErrorInvalidValue;
 }
 
@@ -351,15 +380,20 @@ hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int 
   return hipGetLastError();
 }
 
-int diff_attention_splits(int n_q, int n_k, int B, int heads, int d_head, uint64_t partial_bytes, int cus) {
-  const int64_t tiles = (int64_t)B * ((n_q + (int64_t)B * kTileQ - 1) / ((int64_t)B * kTileQ)) * heads;
-  const int64_t units = (n_k / B + kUnitKeys - 1) / kUnitKeys;
-  const int64_t row = (int64_t)n_q * heads * (4 * d_head + 4) * 4;
-  int64_t splits = std::min<int64_t>({2 * cus / std::max<int64_t>(1, tiles), units / 8, (int64_t)(partial_bytes / std::max<int64_t>(1, row)), 128});
-  return (int)std::max<int64_t>(1, splits);
+void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus) {
+  a.tiles = use_bf16 && (int64_t)rows_q * a.heads >= (int64_t)64 * cus;
+  a.wide = false;
+  a.splits = 1;
+  if (a.tiles) return;
+  const int64_t per_frame = (rows_q + a.B - 1) / a.B, groups = a.B * ((per_frame + kTileQ - 1) / kTileQ) * a.heads;
+  const int64_t units = (rows_k / a.B + kUnitKeys - 1) / kUnitKeys;
+  a.wide = use_bf16 && groups <= cus && units >= 16;
+  const int waves = a.wide ? 8 : 4, places = use_bf16 && !a.wide ? 2 * cus : cus;
+  if (units <= 4 * waves) return;
+  const int64_t row = (int64_t)a.n_q * a.heads * (4 * d_head + 4) * 4;
+  const int64_t splits = std::min<int64_t>({places / std::max<int64_t>(1, groups), units / waves, (int64_t)(partial_bytes / std::max<int64_t>(1, row)), kMostSplits});
+  a.splits = (int)std::max<int64_t>(1, splits);
 }
-
-bool diff_attention_tiles(int n_q, int heads, bool use_bf16, int cus) { return use_bf16 && (int64_t)n_q * heads >= (int64_t)64 * cus; }
 
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s) {
   if (use_bf16 && a.tiles) return launch_diff_tiles(a, d_head, s);

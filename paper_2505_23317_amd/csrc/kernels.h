@@ -447,7 +447,7 @@ hipError_t launch_cell_positions(const int32_t* first, int n_first, const int32_
 // Differential attention of the rows of B <= 64 frames (cu_q) over those of the same frames (cu_k), the first kv_len[f] of
 // them where it is given, the kv_len[f] that key_list names (rows within the frame, from cu_k[f] on) where that is
 // given too.  Offsets that are none set *err_flag and nothing is written.  partial: room for
-// diff_attention_splits' partial results (splits > 1).  Logits are scaled by scale2 in base 2.
+// the splits' partial results (splits > 1).  Logits are scaled by scale2 in base 2.
 struct DiffAttentionArgs {
   const void *q, *k, *v;
   void* out;
@@ -459,15 +459,16 @@ struct DiffAttentionArgs {
   const float *lambda, *head_g;
   float scale2, eps;
   int heads;   // differential heads
-  bool tiles;  // diff_attention_tiles
+  bool tiles;  // plan_diff_attention's: 128 queries a workgroup, or 32 by four wavefronts or (wide) eight
+  bool wide;
   int splits;
   float* partial;
   int32_t* err_flag;
 };
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
-// Whether about n_q query rows go to the kernel of 128 queries a workgroup, and else into how many runs the keys are cut.
-bool diff_attention_tiles(int n_q, int heads, bool use_bf16, int cus);
-int diff_attention_splits(int n_q, int n_k, int B, int heads, int d_head, uint64_t partial_bytes, int cus);
+// Chooses the kernel and its cut for about rows_q query and rows_k key rows (the fields tiles, wide and splits; n_q, B and heads are
+// set); partial_bytes: what a.partial has room for.
+void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus);
 // list, kv_len: the keys of every frame whose mask byte is not 0, for launch_diff_attention.
 hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int n_k, int32_t* list, int32_t* kv_len, hipStream_t s);
 
