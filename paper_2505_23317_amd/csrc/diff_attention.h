@@ -32,20 +32,22 @@ __device__ __forceinline__ Frames frames_of(const int32_t* __restrict__ cu_q, co
   f.bad = __any(bad || (l == 0 && (f.q[0] != 0 || f.k[0] != 0)));
   return f;
 }
-// The frame that piece `id` belongs to, where a frame has pieces[0 or 1] of them (lane's two frames); `id` becomes
-// the piece's number within it.  -1: there are fewer.
-__device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int& id) {
-  const int lane = threadIdx.x & 63;
-  // inclusive sum over the lanes, inside the vector unit: within rows of 16, then row 0 into 1 and 2 into 3, then 1 into 2 and 3
-  int upto = pieces[0] + pieces[1];
-  auto from = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, upto, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+// Sum of v over this lane and those before it: inside the vector unit, within rows of 16, then row 0 into 1 and 2 into 3,
+// then 1 into 2 and 3.
+__device__ __forceinline__ int sum_upto(int v) {
+  auto from = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
   const auto all = std::integral_constant<int, 0xF>{};
-  upto += from(std::integral_constant<int, 0x111>{}, all);   // row_shr:1, 2, 4, 8
-  upto += from(std::integral_constant<int, 0x112>{}, all);
-  upto += from(std::integral_constant<int, 0x114>{}, all);
-  upto += from(std::integral_constant<int, 0x118>{}, all);
-  upto += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
-  upto += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
+  v += from(std::integral_constant<int, 0x111>{}, all);   // row_shr:1, 2, 4, 8
+  v += from(std::integral_constant<int, 0x112>{}, all);
+  v += from(std::integral_constant<int, 0x114>{}, all);
+  v += from(std::integral_constant<int, 0x118>{}, all);
+  v += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
+  v += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
+  return v;
+}
+// The frame that piece `id` belongs to, where a frame has pieces[0 or 1] of them (lane's two frames, `upto` their sum_upto); `id`
+// becomes the piece's number within it.  -1: there are fewer.
+__device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int upto, int& id) {
   const uint64_t in = __ballot(upto > id);
   if (in == 0) return -1;
   const int l = __ffsll((unsigned long long)in) - 1;
@@ -54,6 +56,10 @@ __device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int& id) {
   if (id < first) return 2 * l;
   id -= first;
   return 2 * l + 1;
+}
+__device__ __forceinline__ int of_lane_pair(const int (&values)[2], int frame) {
+  const int even = __builtin_amdgcn_readlane(values[0], frame >> 1), odd = __builtin_amdgcn_readlane(values[1], frame >> 1);
+  return (frame & 1) ? odd : even;
 }
 __device__ __forceinline__ int of_frame(const int (&offsets)[3], int frame) {
   const int even = __builtin_amdgcn_readlane(offsets[0], frame >> 1), odd = __builtin_amdgcn_readlane(offsets[1], frame >> 1);
@@ -163,7 +169,7 @@ __device__ __forceinline__ void unit_logits(const unsigned char* sK, const uint4
 }
 // The reference of the weights follows the largest logit only once that is kSlack ahead (2^kSlack times the
 // others): a quotient is the same for any reference, and with 32 queries in a wavefront some largest logit moves in almost every
-// unit, which costs two operations for every sum (attention of 300 queries a frame, 1600 to 6400 tokens: 33 -> XX us).
+// unit, which costs two operations for every sum (4 frames of 300 queries over 1600 to 6400 tokens: 43 -> 41.7 us).
 constexpr float kSlack = 16.f;
 template <typename T, int MO>
 __device__ __forceinline__ void unit_weights(f32x16 (&s)[2], int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][MO]) {

@@ -3,9 +3,19 @@
 // A workgroup has 128 queries of one head and frame, a wavefront 32 of them, a query is a lane (S^T = K Q^T,
 // O^T = V^T P^T, as in attention.hip).  Both maps of a head are worked out in one pass over the keys, because their
 // values are the same: an operand of the values read from LDS feeds a product of each.  Units of 32 keys go
-// from global memory straight into LDS, keys two stages and values one stage ahead of their use, one barrier a stage.
+// from global memory straight into LDS, two stages before they are waited for, one barrier a stage.
 // Stage u: on the matrix unit the values of unit u - 1 under both maps (16 products at head width 64) and then the
 // logits of unit u + 1 (8), between them the exponentials of unit u, in an order that the compiler is not to change.
+//
+// What bounds it is a SIMD's issue: per stage and wavefront 24 products of 32 clocks' pipe and 1024 exponentials, sums and
+// roundings, which two wavefronts overlap.  Two logits and twice the values make 12 d_head operations a key, query and head: 8 frames of
+// 6400 tokens, 3 heads of width 64, are 7.5e11 of them in 690 us, 1.09e15 a second, where a large product of matrices
+// reaches 1.2e15.
+//
+// KG = 1: four wavefronts, two workgroups a CU.  KG = 2: eight, where those leave CUs with one workgroup: the even
+// and the odd units of keys of the same queries, whose sums and rows (they have the same reference) are added at the end.
+// us, KG 1 / 2, heads of width 64, frames of 6784 tokens, 159 tiles: 155 / 137; 228 tiles of 9728 tokens 230 / 213; 255 of 10,880 271 / 256;
+// 270 (more than CUs) 404 / 471; 348 551 / 604; 4 frames, 96 tiles 26 / 26 (a tile of 32 queries there), 252 80.7 / 75.4, 300 125 / 145.
 //
 // Values lie in memory row by row.  The second product wants, for a lane's column, eight consecutive keys:
 // the transposing LDS read gives four a lane, so no copy of the values by columns is made.
@@ -20,16 +30,21 @@ namespace cfdetr {
 namespace {
 
 constexpr int kTileQ = 128;
-constexpr int kKeySlots = 3, kValueSlots = 4;
+constexpr int kAhead = 2;   // stages that a unit's loads have ahead of them
+// LDS of a workgroup: the stages' keys and values.  Up to 64 KB it is declared with its size, and its addresses are
+// constants: 1 % of the time with four wavefronts.
+template <int DH, int KG>
+constexpr int kStages = (2 * kAhead + 3) * KG * kUnitKeys * 4 * DH;
+template <int DH, int KG>
+constexpr bool kFixed = kStages<DH, KG> <= 63 * 1024;
 constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p+100f;
 
 // A row of queries is finished: the difference of its maps, its norm, its type.  Lane l and l ^ 32 hold the columns
 // 32 i + 8 r + 4 g on of a query; a swap between them makes runs of eight.
 template <int DH>
 __device__ __forceinline__ void finish_rows(const f32x16 (&acc)[2][DH / 16], const float (&l)[2], float lambda, const float* __restrict__ head_g,
-                                            float eps, bf16_t* orow, bool write) {
+                                            float eps, bf16_t* orow, int g, bool write) {
   constexpr int W = 2 * DH, MO = W / 32;
-  const int g = (threadIdx.x & 63) >> 5;
   const float i0 = l[0] != 0.f ? 1.0f / l[0] : 0.f, i1 = l[1] != 0.f ? lambda / l[1] : 0.f;
   f32x16 o[MO];
   float sq = 0.f;
@@ -69,12 +84,12 @@ __device__ __forceinline__ void finish_rows(const f32x16 (&acc)[2][DH / 16], con
 
 // The rare path: a workgroup's queries again, with a running maximum; only those with `again` are written.  A
 // function of its own, so that the registers of the other path are not its business.
-template <int DH>
+template <int DH, int THREADS>
 __device__ __attribute__((noinline)) void redo_rows(const bf16_t* qrow, const bf16_t* kbase, int k_ld, const bf16_t* vbase, int v_ld,
                                                     const int32_t* list, int nk, float scale2, float lambda, const float* head_g, float eps,
                                                     bf16_t* orow, bool again, unsigned char* smem) {
   constexpr int W = 2 * DH, ROWB = 2 * W, CPR = ROWB / 16, KS = CPR / 4, MO = W / 32, UNIT = kUnitKeys * ROWB;
-  const int tid = threadIdx.x, g = (tid & 63) >> 5;
+  const int tid = threadIdx.x, g = (tid & 63) >> 5;   // (wavefronts of the same queries do the same; `again` is set in one)
   unsigned char* const sK = smem;
   unsigned char* const sV = smem + UNIT;
   uint4 qf[2][KS];
@@ -93,7 +108,7 @@ __device__ __attribute__((noinline)) void redo_rows(const bf16_t* qrow, const bf
 #pragma nounroll
   for (int k0 = 0; k0 < nk; k0 += kUnitKeys) {
     __syncthreads();
-    for (int p = tid; p < kUnitKeys * CPR; p += kThreads) {
+    for (int p = tid; p < kUnitKeys * CPR; p += THREADS) {
       const int key = p / CPR, c = p % CPR, at = k0 + key, row = swap_bits_2_3(key);
       uint4 kk = make_uint4(0, 0, 0, 0), vv = kk;
       if (at < nk) {
@@ -111,7 +126,7 @@ __device__ __attribute__((noinline)) void redo_rows(const bf16_t* qrow, const bf
     unit_rows<bf16_t, DH>(sV, s, acc);
   }
   const float l[2] = {half_sum(l_run[0]), half_sum(l_run[1])};
-  finish_rows<DH>(acc, l, lambda, head_g, eps, orow, again);
+  finish_rows<DH>(acc, l, lambda, head_g, eps, orow, g, again);
 }
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -159,14 +174,27 @@ __device__ __forceinline__ Item item_of(const Frames& fr, const int32_t* __restr
   return item;
 }
 
-template <int DH, bool LIST, bool SCALED>
-__global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionArgs a) {
+// This lane's number, counted anew: the compiler cannot carry it, or what is made of it, through the loop, which has no
+// registers for it.
+__device__ __forceinline__ int lane_again() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
+template <int DH, bool LIST, bool SCALED, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void diff_tiles_kernel(DiffAttentionArgs a) {
   constexpr int W = 2 * DH, ROWB = 2 * W, CPR = ROWB / 16;
   constexpr int KS = DH / 16, MO = W / 32;
   constexpr int UNIT = kUnitKeys * ROWB, NI = UNIT / 4096, RPI = 1024 / ROWB;   // a wavefront's loads of a unit, rows of one
   constexpr int NOP = 2 * MO;                       // operands of the values of a unit
   constexpr int NPV = 2 * NOP, NQK = 2 * KS;        // products of a stage
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[(kKeySlots + kValueSlots) * UNIT];
+  constexpr int AHEAD = kAhead, kKeySlots = AHEAD + 1, kValueSlots = AHEAD + 2;
+  constexpr int STAGE = KG * kUnitKeys, BYTES = KG * UNIT;   // keys of a stage, and LDS of those (and of their values)
+  extern __shared__ __attribute__((aligned(1024))) unsigned char sized[];
+  __shared__ __attribute__((aligned(1024))) unsigned char fixed[kFixed<DH, KG> ? kStages<DH, KG> : 16];
+  unsigned char* const smem = kFixed<DH, KG> ? fixed : sized;
+  __shared__ float s_l[KG == 2 ? 2 : 1][4][32];
 
   const Frames fr = frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k);
   if (fr.bad) {
@@ -176,27 +204,25 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   const Item item = item_of(fr, a.kv_len, a.B, a.heads);
   if (item.frame < 0) return;
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, odd = KG == 2 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
   const int frame = __builtin_amdgcn_readfirstlane(item.frame), head = __builtin_amdgcn_readfirstlane(item.head);
   const int q0 = of_frame(fr.q, frame), nq = behind_frame(fr.q, frame) - q0;
   const int k0 = of_frame(fr.k, frame), nk_all = behind_frame(fr.k, frame) - k0;
   const int nk = a.kv_len ? min(nk_all, a.kv_len[frame]) : nk_all;
-  const int q_local = __builtin_amdgcn_readfirstlane(item.tile) * kTileQ + wave * 32 + l32;
-  const bool mine = q_local < nq;
-  const size_t q_row = (size_t)(q0 + min(q_local, nq - 1));
-  const bf16_t* const qrow = static_cast<const bf16_t*>(a.q) + q_row * a.q_ld + head * W;
-  bf16_t* const orow = static_cast<bf16_t*>(a.out) + q_row * a.out_ld + head * W;
+  const int q_first = __builtin_amdgcn_readfirstlane(item.tile) * kTileQ + wave * 32, q_local = q_first + l32;
+  const bf16_t* qrow = static_cast<const bf16_t*>(a.q) + (size_t)(q0 + min(q_local, nq - 1)) * a.q_ld + head * W;
   const bf16_t* const kbase = static_cast<const bf16_t*>(a.k) + (size_t)k0 * a.k_ld + head * W;
   const bf16_t* const vbase = static_cast<const bf16_t*>(a.v) + (size_t)k0 * a.v_ld + head * W;
   const int32_t* const list = LIST ? a.key_list + k0 : nullptr;
   const float lambda = a.lambda[head];
-  const int n = (nk + kUnitKeys - 1) / kUnitKeys;
+  const int n = (nk + STAGE - 1) / STAGE;   // stages
   if (n == 0) {
-    if (mine)
-      for (int c = g; c < CPR; c += 2) *reinterpret_cast<uint4*>(orow + 8 * c) = make_uint4(0, 0, 0, 0);
+    bf16_t* const orow = static_cast<bf16_t*>(a.out) + (size_t)(q0 + q_local) * a.out_ld + head * W;
+    if (q_local < nq)
+      for (int c = 2 * odd + g; c < CPR; c += 2 * KG) *reinterpret_cast<uint4*>(orow + 8 * c) = make_uint4(0, 0, 0, 0);
     return;
   }
-  const int ragged = nk & (kUnitKeys - 1);   // keys of a last unit that is not full
+  const int ragged = nk & (STAGE - 1);   // keys of a last stage that is not full
 
   bf16x8 qf[2][KS];
 #pragma unroll
@@ -204,49 +230,55 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[m][ks] = *reinterpret_cast<const bf16x8*>(qrow + m * DH + ks * 16 + g * 8);
 
-  // Loads: piece `lane` of instruction j of this wavefront lies in LDS row (wave NI + j) RPI + lane / CPR; which key and
-  // chunk that is, is the order of the rows and chunks in LDS.
+  // Loads: piece `lane` of load j lies in LDS row (wave NI + j) RPI + lane / CPR; which key and chunk that is, is the order of
+  // the rows and chunks in LDS.  Two loads of a wavefront are four rows apart: eight keys, with the same chunks of
+  // the values.  The offsets of full units are kept, what else is asked for is worked out where it is.
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-  int key[NI];
-  uint32_t k_col[NI], v_col[NI];
-#pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    const int rho = (wave * NI + j) * RPI + lane / CPR, c = lane % CPR;
-    key[j] = swap_bits_2_3(rho);
-    k_col[j] = key_piece<bf16_t, ROWB>(rho, c) * 16;
-    v_col[j] = value_piece<bf16_t, ROWB>(rho, c) * 16;
-  }
-  auto load = [&](const bf16_t* base, int ld, const uint32_t(&col)[NI], int u, uint32_t to) {
-    to += wave * (NI * 1024);
-    if constexpr (LIST) {
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const size_t row = list[min(u * kUnitKeys + key[j], nk - 1)];
-        dma16(reinterpret_cast<const char*>(base) + row * (size_t)ld * 2 + col[j], to + j * 1024);
+  auto row_of = [&](int l, int j) { return (wave * NI + j) * RPI + l / CPR; };
+  auto column = [&](int l, int j, auto values) {
+    const int rho = row_of(l, j), c = l % CPR;
+    return (uint32_t)(decltype(values)::value ? value_piece<bf16_t, ROWB>(rho, c) : key_piece<bf16_t, ROWB>(rho, c)) * 16;
+  };
+  const auto of_keys = std::integral_constant<bool, false>{};
+  const auto of_values = std::integral_constant<bool, true>{};
+  static_assert(NI == 1 || (NI == 2 && RPI == 4), "the second load's keys are eight behind the first's");
+  const uint32_t k_off = (uint32_t)swap_bits_2_3(row_of(lane, 0)) * (uint32_t)(a.k_ld * 2) + column(lane, 0, of_keys);
+  const uint32_t v_off = (uint32_t)swap_bits_2_3(row_of(lane, 0)) * (uint32_t)(a.v_ld * 2) + column(lane, 0, of_values);
+  auto load = [&](const bf16_t* base, int ld, auto values, int stage, uint32_t to) {
+    to += odd * UNIT + wave * (NI * 1024);
+    const int first = (KG * stage + odd) * kUnitKeys;
+    if (!LIST && first + kUnitKeys <= nk) {
+      const bf16_t* const from = base + (size_t)first * ld;
+      dma16(from, decltype(values)::value ? v_off : k_off, to);
+      if constexpr (NI == 2) {
+        // eight keys on; the keys' chunks of rows four on: bit 2 of their number turned.  Four wavefronts have the registers to
+        // keep that, 1.5 % of their time.
+        const uint32_t off = decltype(values)::value ? v_off : k_off + 64 - (uint32_t)(((KG == 1 ? lane : lane_again()) & 4) << 5);
+        if constexpr (KG == 1) dma16(from, off + (uint32_t)(16 * ld), to + 1024);
+        else dma16(from + (size_t)8 * ld, off, to + 1024);
       }
     } else {
-      const bf16_t* const from = base + (size_t)(u * kUnitKeys) * ld;
-      const int last = nk - 1 - u * kUnitKeys;   // (rows behind the last key are the last key's, and are not used)
-      if (last >= kUnitKeys - 1) {
+      // rows behind the last key are the last key's, and are not used
+      const int l = lane_again();
 #pragma unroll
-        for (int j = 0; j < NI; ++j) dma16(from, (uint32_t)key[j] * (uint32_t)(ld * 2) + col[j], to + j * 1024);
-      } else {
-#pragma unroll
-        for (int j = 0; j < NI; ++j) dma16(from, (uint32_t)min(key[j], last) * (uint32_t)(ld * 2) + col[j], to + j * 1024);
+      for (int j = 0; j < NI; ++j) {
+        const int at = min(first + swap_bits_2_3(row_of(l, j)), nk - 1);
+        const size_t row = LIST ? list[at] : at;
+        dma16(reinterpret_cast<const char*>(base) + row * (size_t)ld * 2 + column(l, j, values), to + j * 1024);
       }
     }
   };
-  auto slot = [](int u, int slots) { return (uint32_t)(u % slots) * UNIT; };
-  constexpr uint32_t VALUES = kKeySlots * UNIT;
-  auto load_k = [&](int u, uint32_t at) { load(kbase, a.k_ld, k_col, u, lds0 + at); };
-  auto load_v = [&](int u, uint32_t at) { load(vbase, a.v_ld, v_col, u, lds0 + VALUES + at); };
+  auto slot = [](int u, int slots) { return (uint32_t)(u % slots) * BYTES; };
+  constexpr uint32_t VALUES = kKeySlots * BYTES;
+  auto load_k = [&](int u, uint32_t at) { load(kbase, a.k_ld, of_keys, u, lds0 + at); };
+  auto load_v = [&](int u, uint32_t at) { load(vbase, a.v_ld, of_values, u, lds0 + VALUES + at); };
 
   // Operands: row l32 of the keys, chunk 2 ks + g of a map; for the values the transposing read's pieces.
-  const uint32_t k_at = l32 * ROWB + key_chunk<bf16_t, ROWB>(l32, g) * 16;
+  const uint32_t k_at = odd * UNIT + l32 * ROWB + key_chunk<bf16_t, ROWB>(l32, g) * 16;
   const int v_row = 4 * g + ((lane & 15) >> 2);   // of keys 8 g on; those of 8 g + 4 on are 8 rows behind
-  const uint32_t v_at = VALUES + v_row * ROWB + value_block<bf16_t, ROWB>(v_row, 0) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-  auto read_k = [&](uint32_t at, int kk) {   // operand kk = 2 ks + map (chunks and blocks are moved by bits: an exclusive or)
-    return *reinterpret_cast<const bf16x8*>(smem + ((at + k_at) ^ (uint32_t)(((kk & 1) * 2 * KS + 2 * (kk >> 1)) * 16)));
+  const uint32_t v_at = VALUES + odd * UNIT + v_row * ROWB + value_block<bf16_t, ROWB>(v_row, 0) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  auto read_k = [&](uint32_t at, int kk) {   // operand kk = KS map + ks (chunks and blocks are moved by bits: an exclusive or)
+    return *reinterpret_cast<const bf16x8*>(smem + ((at + k_at) ^ (uint32_t)(2 * kk * 16)));
   };
   auto read_v = [&](uint32_t at, int p) {   // operand p = 2 block + half of the unit's keys
     union {
@@ -272,7 +304,7 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   bf16x8 vb[3], kb[3];
 
   auto qk = [&](f32x16(&s)[2], const bf16x8& k, int kk) {
-    const int m = kk & 1, ks = kk >> 1;
+    const int m = kk / KS, ks = kk % KS;
     if (ks == 0) {
       f32x16 z;
 #pragma unroll
@@ -283,24 +315,36 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
     }
   };
   auto mask = [&](f32x16(&s)[2]) {
+    const int g = lane_again() >> 5, left = ragged - odd * kUnitKeys;   // (an odd unit may have none)
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (16 * (r >> 3) + 8 * g + (r & 7) >= ragged) s[m][r] = -INFINITY;
+        if (16 * (r >> 3) + 8 * g + (r & 7) >= left) s[m][r] = -INFINITY;
   };
-  // In front of stage u: its keys' successors and its values are in LDS, everyone is past stage u - 1, and
-  // the slots that that has left are filled.
+  // In front of stage u: the keys of unit u + 1 and the values of unit u, asked for AHEAD stages before, are in LDS, everyone is
+  // past stage u - 1, and the slots that that has left are filled.  What may still be on its way is what the
+  // stages between have asked for, in the last ones less.
   auto begin = [&](int u) {
-    if (u + 2 < n) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(2 * NI) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
-    if (u + 3 < n) load_k(u + 3, slot(u, kKeySlots));
-    if (u + 2 < n) load_v(u + 2, slot(u + 2, kValueSlots));
+    const int left = n - (u + AHEAD);
+    auto wait = [](auto units) {
+      constexpr int kUnits = decltype(units)::value > 0 ? decltype(units)::value : 0;
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kUnits * NI) : "memory");
+    };
+    constexpr int FULL = 2 * (AHEAD - 1);
+    if (left > 0) wait(std::integral_constant<int, FULL>{});
+    else if (left == 0) wait(std::integral_constant<int, FULL - 1>{});
+    else if (left == -1) wait(std::integral_constant<int, FULL - 3>{});
+    else if (left == -2) wait(std::integral_constant<int, FULL - 5>{});
+    else if (left == -3) wait(std::integral_constant<int, FULL - 7>{});
+    else wait(std::integral_constant<int, 0>{});
+    if (u + AHEAD + 1 < n) load_k(u + AHEAD + 1, slot(u, kKeySlots));
+    if (u + AHEAD < n) load_v(u + AHEAD, slot(u + AHEAD, kValueSlots));
   };
   auto stage = [&](f32x16(&s)[2], f32x16(&sn)[2], bf16x8(&pc)[2][2], bf16x8(&pp)[2][2], int u, auto more_tag) {
     constexpr bool kMore = decltype(more_tag)::value;   // there is a unit u + 1
     constexpr int NM = NPV + (kMore ? NQK : 0), PAIRS = 16;
-    const uint32_t v_prev = slot(u - 1 + kValueSlots, kValueSlots), v_this = slot(u, kValueSlots), k_next = slot(u + 1, kKeySlots);
+    const uint32_t v_prev = slot(u + kValueSlots - 1, kValueSlots), v_this = slot(u, kValueSlots), k_next = slot(u + 1, kKeySlots);
     uint32_t w[2][8];
     float e0 = 0.f, e1 = 0.f, sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -353,26 +397,29 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   const auto yes = std::integral_constant<bool, true>{};
   const auto no = std::integral_constant<bool, false>{};
 
+  // in the order in which they are waited for
   load_k(0, slot(0, kKeySlots));
-  load_v(0, slot(0, kValueSlots));
-  if (n > 1) {
-    load_k(1, slot(1, kKeySlots));
-    load_v(1, slot(1, kValueSlots));
+#pragma nounroll
+  for (int u = 0; u < AHEAD && u < n; ++u) {
+    if (u + 1 < n) load_k(u + 1, slot(u + 1, kKeySlots));
+    load_v(u, slot(u, kValueSlots));
   }
-  if (n > 2) load_k(2, slot(2, kKeySlots));
   // In front of the first unit: values of a unit before it, all 0, met with probabilities 0.
-  for (int p = tid; p < UNIT / 16; p += kThreads) *reinterpret_cast<uint4*>(smem + VALUES + slot(kValueSlots - 1, kValueSlots) + p * 16) = make_uint4(0, 0, 0, 0);
+  for (int p = tid; p < BYTES / 16; p += 256 * KG) *reinterpret_cast<uint4*>(smem + VALUES + slot(kValueSlots - 1, kValueSlots) + p * 16) = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int e = 0; e < 8; ++e) vb[0][e] = vb[1][e] = pA[0][0][e] = pA[0][1][e] = pA[1][0][e] = pA[1][1][e] = (__bf16)0.f;
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+  if (n >= AHEAD) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((2 * AHEAD - 1) * NI) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
   // The last unit: keys behind the frame's have no weight, and their values are cleared (0 times what they are copies of
   // may be no number).
   auto last = [&](f32x16(&s)[2]) {
     if (ragged == 0) return;
     mask(s);
     const uint32_t at = VALUES + slot(n - 1, kValueSlots);
-    for (int p = tid; p < (kUnitKeys - ragged) * CPR; p += kThreads)
-      *reinterpret_cast<uint4*>(smem + at + swap_bits_2_3(ragged + p / CPR) * ROWB + p % CPR * 16) = make_uint4(0, 0, 0, 0);
+    for (int p = (4 * odd + wave) * 64 + lane_again(); p < (STAGE - ragged) * CPR; p += 256 * KG) {
+      const int key = ragged + p / CPR;
+      *reinterpret_cast<uint4*>(smem + at + (key & kUnitKeys) / kUnitKeys * UNIT + swap_bits_2_3(key & (kUnitKeys - 1)) * ROWB + p % CPR * 16) = make_uint4(0, 0, 0, 0);
+    }
     __syncthreads();
   };
   auto final_pv = [&](bf16x8(&p)[2][2]) {
@@ -411,30 +458,76 @@ __global__ __launch_bounds__(kThreads, 2) void diff_tiles_kernel(DiffAttentionAr
   stage(sA, sB, pA, pB, u, no);
   final_pv(pA);
 
-  const float l[2] = {half_sum(l_run[0]), half_sum(l_run[1])};
-  const bool again = !(l[0] >= kSumLow && l[0] <= kSumHigh && l[1] >= kSumLow && l[1] <= kSumHigh);
-  finish_rows<DH>(acc, l, lambda, a.head_g, a.eps, orow, mine && !again);
-  if (__syncthreads_or(mine && again))
-    redo_rows<DH>(qrow, kbase, a.k_ld, vbase, a.v_ld, list, nk, a.scale2, lambda, a.head_g, a.eps, orow, mine && again, smem);
+  // The odd units' sums and rows to the wavefront with the even ones, one map after the other; that one finishes its queries' rows
+  // (where they lie is worked out again: the loop has no registers for it).
+  const int lane_end = lane_again();
+  float l[2] = {half_sum(l_run[0]), half_sum(l_run[1])};
+  if constexpr (KG == 2) {
+    if (odd && lane_end < 32) {
+      s_l[0][wave][lane_end] = l[0];
+      s_l[1][wave][lane_end] = l[1];
+    }
+    float4* const rows = reinterpret_cast<float4*>(smem) + wave * (MO * 4 * 64) + lane_end;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      __syncthreads();
+      if (odd) {
+#pragma unroll
+        for (int i = 0; i < MO; ++i)
+#pragma unroll
+          for (int rq = 0; rq < 4; ++rq)
+            rows[(4 * i + rq) * 64] = make_float4(acc[m][i][4 * rq], acc[m][i][4 * rq + 1], acc[m][i][4 * rq + 2], acc[m][i][4 * rq + 3]);
+      }
+      __syncthreads();
+      if (!odd) {
+#pragma unroll
+        for (int i = 0; i < MO; ++i)
+#pragma unroll
+          for (int rq = 0; rq < 4; ++rq) {
+            const float4 v = rows[(4 * i + rq) * 64];
+            acc[m][i][4 * rq] += v.x;
+            acc[m][i][4 * rq + 1] += v.y;
+            acc[m][i][4 * rq + 2] += v.z;
+            acc[m][i][4 * rq + 3] += v.w;
+          }
+        l[m] += s_l[m][wave][lane_end & 31];
+      }
+    }
+  }
+  const int q_again = q_first + (lane_end & 31);
+  const bool mine = !odd && q_again < nq;
+  const size_t q_row = (size_t)(q0 + min(q_again, nq - 1));
+  qrow = static_cast<const bf16_t*>(a.q) + q_row * a.q_ld + head * W;
+  bf16_t* const orow = static_cast<bf16_t*>(a.out) + q_row * a.out_ld + head * W;
+  const bool again = mine && !(l[0] >= kSumLow && l[0] <= kSumHigh && l[1] >= kSumLow && l[1] <= kSumHigh);
+  if (!odd) finish_rows<DH>(acc, l, lambda, a.head_g, a.eps, orow, lane_end >> 5, mine && !again);
+  if (__syncthreads_or(again))
+    redo_rows<DH, 256 * KG>(qrow, kbase, a.k_ld, vbase, a.v_ld, list, nk, a.scale2, lambda, a.head_g, a.eps, orow, again, smem);
 }
 
-template <int DH>
+template <int DH, bool LIST, bool SCALED, int KG>
 hipError_t go(const DiffAttentionArgs& a, hipStream_t s) {
+  constexpr int LDS = kFixed<DH, KG> ? 0 : kStages<DH, KG>;
+  static_assert(KG == 1 || kStages<DH, KG> >= 4 * 32 * 2 * DH * 4, "the odd units' rows of a map");
+  static DeviceOnce once;
+  if (LDS > 0)
+    if (hipError_t e = allow_lds(diff_tiles_kernel<DH, LIST, SCALED, KG>, LDS, &once); e != hipSuccess) return e;
   const int64_t items = ((int64_t)a.n_q / kTileQ + a.B) * a.heads;
-  const dim3 grid((unsigned)(8 * (items / 8 + a.B + 1)));
-  const bool scaled = a.scale2 != 1.0f;
-  if (a.key_list && scaled) hipLaunchKernelGGL((diff_tiles_kernel<DH, true, true>), grid, dim3(kThreads), 0, s, a);
-  else if (a.key_list) hipLaunchKernelGGL((diff_tiles_kernel<DH, true, false>), grid, dim3(kThreads), 0, s, a);
-  else if (scaled) hipLaunchKernelGGL((diff_tiles_kernel<DH, false, true>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((diff_tiles_kernel<DH, false, false>), grid, dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((diff_tiles_kernel<DH, LIST, SCALED, KG>), dim3((unsigned)(8 * (items / 8 + a.B + 1))), dim3(256 * KG), LDS, s, a);
   return hipGetLastError();
+}
+template <int DH, int KG>
+hipError_t go(const DiffAttentionArgs& a, hipStream_t s) {
+  const bool scaled = a.scale2 != 1.0f;
+  if (a.key_list) return scaled ? go<DH, true, true, KG>(a, s) : go<DH, true, false, KG>(a, s);
+  return scaled ? go<DH, false, true, KG>(a, s) : go<DH, false, false, KG>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_diff_tiles(const DiffAttentionArgs& a, int d_head, hipStream_t s) {
-  if (d_head == 64) return go<64>(a, s);
-  if (d_head == 32) return go<32>(a, s);
+  if (d_head == 64) return a.wide ? go<64, 2>(a, s) : go<64, 1>(a, s);
+  if (d_head == 32) return a.wide ? go<32, 2>(a, s) : go<32, 1>(a, s);
   return hipErrorInvalidValue;
 }
 

@@ -459,8 +459,7 @@ struct DiffAttentionArgs {
   const float *lambda, *head_g;
   float scale2, eps;
   int heads;   // differential heads
-  bool tiles;  // plan_diff_attention's: 128 queries a workgroup, or 32 by four wavefronts or (wide) eight
-  bool wide;
+  bool tiles, wide;  // plan_diff_attention's: 128 queries a workgroup or 32, by eight wavefronts (wide) or four
   int splits;
   float* partial;
   int32_t* err_flag;

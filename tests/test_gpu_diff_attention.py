@@ -75,34 +75,40 @@ def test_longer_frames(K, d, n):
 
 
 # Frames of every length about a unit of 32 keys and a tile of 128 queries, often enough for the kernel of many queries (rows times
-# heads from 16,384 on, on 256 CUs), empty ones between them.
+# heads from 16,384 on, on 256 CUs: eight wavefronts a tile, beyond 32,768 four), empty ones between them.
 EDGES = [0, 1, 2, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 0, 160, 255, 256, 257, 300, 513, 0]
 
 
-def _many(d):
+MANY = (20_000, 40_000)
+
+
+def _many(d, rows):
     n, heads = [], T.MODELS[d] // 2
-    while sum(n) * heads < 20_000:
+    while sum(n) * heads < rows:
         n += EDGES
-    return n[:63] + [20_000 // heads - sum(n[:63])] if len(n) > 64 else n
+    return n[:63] + [rows // heads - sum(n[:63])] if len(n) > 64 else n
 
 
 @pytest.mark.parametrize("norm", (True, False))
 @pytest.mark.parametrize("d", (64, 256, 384, 768, 1024))
-def test_many_queries(K, d, norm):
-    n = _many(d)
+@pytest.mark.parametrize("rows", MANY)
+def test_many_queries(K, d, norm, rows):
+    n = _many(d, rows)
     _run(K, d, n, n, norm=norm, scale=0.2 if norm else None)
 
 
 @pytest.mark.parametrize("d", (256, 384))
-def test_many_queries_over_other_rows(K, d):
-    n = _many(d)
+@pytest.mark.parametrize("rows", MANY)
+def test_many_queries_over_other_rows(K, d, rows):
+    n = _many(d, rows)
     _run(K, d, n, [(7 * m + 3) % 211 for m in n])
 
 
 @pytest.mark.parametrize("d,share", [(256, 0.5), (384, 0.1), (384, 0.95)])
-def test_many_queries_masked(K, d, share):
+@pytest.mark.parametrize("rows", MANY)
+def test_many_queries_masked(K, d, share, rows):
     import torch
-    n = _many(d)
+    n = _many(d, rows)
     q, k, v = (x.clone() for x in _inputs(d, n, n, "bf16"))
     g = torch.Generator(device="cuda")
     g.manual_seed(9)
@@ -164,7 +170,8 @@ def test_masks_that_leave_everything_or_nothing(K):
     enc.close()
 
 
-@pytest.mark.parametrize("n", ([1, 63, 64, 65, 129, 200, 1000], [1500] * 2, [1, 63, 65, 129, 200, 1000] * 6))
+@pytest.mark.parametrize("n", ([1, 63, 64, 65, 129, 200, 1000], [1500] * 2, [1, 63, 65, 129, 200, 1000] * 6,
+                               [1, 63, 65, 129, 200, 1000] * 10))
 @pytest.mark.parametrize("level", (-400.0, -90.0, 90.0, 400.0))
 @pytest.mark.parametrize("d", (256, 384))
 def test_logits_far_from_zero(K, d, n, level):
@@ -227,20 +234,21 @@ def test_no_numbers_stay_in_their_frame(K):
 
 
 @pytest.mark.parametrize("d", (256, 384))
-def test_no_numbers_among_many_queries(K, d):
+@pytest.mark.parametrize("more", (0, 6001))
+def test_no_numbers_among_many_queries(K, d, more):
     """A value that is no number reaches its column of the rows of its frame, the last key's too."""
     import torch
-    n = [3000, 129, 3000, 97]
+    n = [3000, 129, 3000, 97] + [more] * (more > 0)
     q, k, v = (x.clone() for x in _inputs(d, n, n, "bf16", std=0.3))
     k[10, 3], v[3000 + 128, 70], v[6129 + 96, 5] = math.nan, math.inf, -math.inf
     w = 2 * d // T.MODELS[d]
-    enc = T.encoder(d, sum(n), 4)
+    enc = T.encoder(d, sum(n), len(n))
     out = torch.empty(sum(n), d, device="cuda").bfloat16()
     enc.diff_attention(q, k, v, T.offsets(n), T.offsets(n), torch.full((T.MODELS[d] // 2,), 0.0, device="cuda"), out)
     bad = ~torch.isfinite(out)
     assert bad[:3000, :w].all() and not bad[:3000, w:].any() and not bad[3129:6129].any()
     assert (out[3000:3129, 70] == math.inf).all() and bad[3000:3129].sum() == 129
-    assert (out[6129:, 5] == -math.inf).all() and bad[6129:].sum() == 97
+    assert (out[6129:6226, 5] == -math.inf).all() and bad[6129:].sum() == 97
     enc.close()
 
 
