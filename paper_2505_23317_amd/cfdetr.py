@@ -447,12 +447,14 @@ def _to_device(arr: np.ndarray, as_bf16: bool):
 _DTYPES: Dict[str, object] = {}
 
 
-def _expect(t, dtype: str, what: str, shape=None) -> None:
-    """A tensor that the library takes as it lies: contiguous, on the GPU, of the named type and shape."""
+def _expect(t, dtype: str, what: str, shape=None, gpu=None) -> None:
+    """A tensor that the library takes as it lies: contiguous, on the GPU (number `gpu`, if given), of the named type and shape."""
     if not _DTYPES:
         import torch
         _DTYPES.update({n: getattr(torch, n) for n in ("float64", "float32", "bfloat16", "int32", "uint8")})
-    if t.dtype is not _DTYPES[dtype] or (shape is not None and t.shape != shape) or not t.is_contiguous() or not t.is_cuda:
+    on = t.get_device()   # (-1: not on a GPU)
+    if (t.dtype is not _DTYPES[dtype] or (shape is not None and t.shape != shape) or not t.is_contiguous() or on < 0
+            or (gpu is not None and on != gpu)):
         raise ValueError(f"{what}: contiguous {dtype} on the GPU expected"
                          + (f", shape {tuple(shape)}" if shape is not None else ""))
 
@@ -506,6 +508,7 @@ class Encoder:
             setattr(w, name, self.dev[name].data_ptr())
         self.c_cfg, self.c_w = c, w
         self.act = torch.bfloat16 if self.act_bf16 else torch.float32
+        self.gpu = self.dev["lnf_g"].get_device()   # number of the context's GPU
         self.ctx = cfdetr_create(c, w)
 
     # -- helpers ---------------------------------------------------------------
@@ -633,8 +636,8 @@ class Encoder:
     def _rows(self, t, shape, what: str) -> int:
         """Elements from row to row of a tensor [rows, d] in act_dtype whose rows are contiguous.  (Every field of a tensor
         is asked for once: the checks of a rotation take 3 us of its 6.9, the library's call 3.8.)"""
-        if t.dtype is not self.act or t.shape != shape or not t.is_cuda:
-            raise ValueError(f"{what}: rows {tuple(shape)} of {self.act} on the GPU expected")
+        if t.dtype is not self.act or t.shape != shape or t.get_device() != self.gpu:
+            raise ValueError(f"{what}: rows {tuple(shape)} of {self.act} on the context's GPU expected")
         step, one = t.stride()
         if one != 1:
             raise ValueError(f"{what}: the elements of a row must lie next to each other")
@@ -645,8 +648,8 @@ class Encoder:
         rows may lie apart (columns of a wider tensor)."""
         shape = (q.shape[0], self.cfg.d)
         M = shape[0]
-        _expect(freq, "float64", "freq", (params.rot_dim // 2,))
-        _expect(pos, "float32", "pos", (M, params.n_axes))
+        _expect(freq, "float64", "freq", (params.rot_dim // 2,), self.gpu)
+        _expect(pos, "float32", "pos", (M, params.n_axes), self.gpu)
         rows = self._rows
         q_ld, qo_ld, k_ld, ko_ld = rows(q, shape, "q"), rows(q_out, shape, "q_out"), 0, 0
         if k is not None or k_out is not None:
@@ -662,13 +665,13 @@ class Encoder:
         float32 [2 d_head] or None; key_mask: uint8 [n_k] or None.  softmax_scale: None for 1 / sqrt(d_head), 0 for
         queries that have been multiplied by log2(e) / sqrt(d_head)."""
         n_q, n_k, B, rows, d = q.shape[0], k.shape[0], cu_q.shape[0] - 1, self._rows, self.cfg.d
-        _expect(cu_q, "int32", "cu_q", (B + 1,))
-        _expect(cu_k, "int32", "cu_k", (B + 1,))
-        _expect(lambda_, "float32", "lambda_", (self.cfg.heads // 2,))
+        _expect(cu_q, "int32", "cu_q", (B + 1,), self.gpu)
+        _expect(cu_k, "int32", "cu_k", (B + 1,), self.gpu)
+        _expect(lambda_, "float32", "lambda_", (self.cfg.heads // 2,), self.gpu)
         if head_g is not None:
-            _expect(head_g, "float32", "head_g", (2 * self.cfg.d_head,))
+            _expect(head_g, "float32", "head_g", (2 * self.cfg.d_head,), self.gpu)
         if key_mask is not None:
-            _expect(key_mask, "uint8", "key_mask", (n_k,))
+            _expect(key_mask, "uint8", "key_mask", (n_k,), self.gpu)
         if softmax_scale is None:
             softmax_scale = self.cfg.d_head ** -0.5
         cfdetr_diff_attention(self.ctx, q.data_ptr(), rows(q, (n_q, d), "q"), n_q, k.data_ptr(),
@@ -683,19 +686,27 @@ class Encoder:
             for name, t in params.tensors.items():
                 if t is not None and name != "cu_seqlens" and t.numel() != (params.B * d if name == "gate" and params.B else d):
                     raise ValueError(f"{name}: {d} columns expected, and a row for every frame of cu_seqlens in the gate")
+                if t is not None and t.get_device() != self.gpu:
+                    raise ValueError(f"{name}: not on the context's GPU")
             params.width = d
         shape = (M, d)
-        _expect(x, "float32", "x", shape)
-        _expect(block, act, "block", shape)
-        _expect(x_out, "float32", "x_out", shape)
+        _expect(x, "float32", "x", shape, self.gpu)
+        _expect(block, act, "block", shape, self.gpu)
+        _expect(x_out, "float32", "x_out", shape, self.gpu)
         if normed is not None:
-            _expect(normed, act, "normed", shape)
+            _expect(normed, act, "normed", shape, self.gpu)
         cfdetr_norm_residual(self.ctx, params, x.data_ptr(), block.data_ptr(), x_out.data_ptr(), _ptr(normed), M,
                              self._stream())
 
     def attach_differential(self, weights: Dict[str, np.ndarray], rotary: CfdetrRotaryParams, res_scale: float = 1.0):
         """weights: float32 numpy arrays named as include/cfdetr.h lists them ("lambda", and any of "head_g",
         "post1_g", "post2_g", "gate1", "gate2"); uploaded here and kept alive with the context."""
+        cfg = self.cfg
+        widths = dict.fromkeys(DIFFERENTIAL_FIELDS, cfg.d)
+        widths.update({"lambda": cfg.heads // 2, "head_g": 2 * cfg.d_head})
+        for name, v in weights.items():
+            if name not in widths or v.shape != (cfg.layers, widths[name]):
+                raise ValueError(f"{name}: one of {DIFFERENTIAL_FIELDS} expected, a row of its width for every layer")
         dev = {k: _to_device(v, False) for k, v in weights.items()}
         w = CfdetrDifferentialWeights()
         for name, t in dev.items():

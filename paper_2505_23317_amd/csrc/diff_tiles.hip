@@ -22,7 +22,8 @@
 //
 // Probabilities are powers of two relative to the reference 0 and not to a running maximum, rounded to bf16 (half
 // a step of 2^-8 each, independent between keys) and summed in 32 bits before that.  A sum outside
-// [2^-64, 2^100], or that is no number, sends its query through a walk with a running maximum (redo_rows).
+// [2^-64, 2^100], or that is no number, and a row that is none, sends its query through a walk with a running
+// maximum (redo_rows).
 #include "diff_attention.h"
 
 namespace cfdetr {
@@ -40,10 +41,11 @@ constexpr bool kFixed = kStages<DH, KG> <= 63 * 1024;
 constexpr float kSumLow = 0x1p-64f, kSumHigh = 0x1p+100f;
 
 // A row of queries is finished: the difference of its maps, its norm, its type.  Lane l and l ^ 32 hold the columns
-// 32 i + 8 r + 4 g on of a query; a swap between them makes runs of eight.
+// 32 i + 8 r + 4 g on of a query; a swap between them makes runs of eight.  False: not written, asked for or because
+// `finite` is and the row's squares are too large for 32 bits or no numbers.
 template <int DH>
-__device__ __forceinline__ void finish_rows(const f32x16 (&acc)[2][DH / 16], const float (&l)[2], float lambda, const float* __restrict__ head_g,
-                                            float eps, bf16_t* orow, int g, bool write) {
+__device__ __forceinline__ bool finish_rows(const f32x16 (&acc)[2][DH / 16], const float (&l)[2], float lambda, const float* __restrict__ head_g,
+                                            float eps, bf16_t* orow, int g, bool write, bool finite) {
   constexpr int W = 2 * DH, MO = W / 32;
   const float i0 = l[0] != 0.f ? 1.0f / l[0] : 0.f, i1 = l[1] != 0.f ? lambda / l[1] : 0.f;
   f32x16 o[MO];
@@ -57,8 +59,10 @@ __device__ __forceinline__ void finish_rows(const f32x16 (&acc)[2][DH / 16], con
       if (lambda != 0.f) o[i][r] = fmaf(-acc[1][i][r], i1, o[i][r]);
       sq = fmaf(o[i][r], o[i][r], sq);
     }
+  sq = half_sum(sq);
+  if (finite && !(sq < INFINITY)) write = false;
   if (head_g) {
-    const float n = rsqrtf(half_sum(sq) * (1.0f / W) + eps);
+    const float n = rsqrtf(sq * (1.0f / W) + eps);
 #pragma unroll
     for (int i = 0; i < MO; ++i)
 #pragma unroll
@@ -80,6 +84,7 @@ __device__ __forceinline__ void finish_rows(const f32x16 (&acc)[2][DH / 16], con
       const u32x2 b = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[i][8 * rp + 2], o[i][8 * rp + 3]), pack_bf16x2(o[i][8 * rp + 6], o[i][8 * rp + 7]), false, false);
       if (write) *reinterpret_cast<uint4*>(orow + 32 * i + 16 * rp + 8 * g) = make_uint4(a[0], b[0], a[1], b[1]);
     }
+  return write;
 }
 
 // The rare path: a workgroup's queries again, with a running maximum; only those with `again` are written.  A
@@ -126,7 +131,7 @@ __device__ __attribute__((noinline)) void redo_rows(const bf16_t* qrow, const bf
     unit_rows<bf16_t, DH>(sV, s, acc);
   }
   const float l[2] = {half_sum(l_run[0]), half_sum(l_run[1])};
-  finish_rows<DH>(acc, l, lambda, head_g, eps, orow, g, again);
+  finish_rows<DH>(acc, l, lambda, head_g, eps, orow, g, again, false);
 }
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
@@ -499,8 +504,9 @@ __global__ __launch_bounds__(256 * KG, 2) void diff_tiles_kernel(DiffAttentionAr
   const size_t q_row = (size_t)(q0 + min(q_again, nq - 1));
   qrow = static_cast<const bf16_t*>(a.q) + q_row * a.q_ld + head * W;
   bf16_t* const orow = static_cast<bf16_t*>(a.out) + q_row * a.out_ld + head * W;
-  const bool again = mine && !(l[0] >= kSumLow && l[0] <= kSumHigh && l[1] >= kSumLow && l[1] <= kSumHigh);
-  if (!odd) finish_rows<DH>(acc, l, lambda, a.head_g, a.eps, orow, lane_end >> 5, mine && !again);
+  const bool in_range = l[0] >= kSumLow && l[0] <= kSumHigh && l[1] >= kSumLow && l[1] <= kSumHigh;
+  bool again = false;
+  if (!odd) again = !finish_rows<DH>(acc, l, lambda, a.head_g, a.eps, orow, lane_end >> 5, mine && in_range, true) && mine;
   if (__syncthreads_or(again))
     redo_rows<DH, 256 * KG>(qrow, kbase, a.k_ld, vbase, a.v_ld, list, nk, a.scale2, lambda, a.head_g, a.eps, orow, again, smem);
 }

@@ -444,7 +444,7 @@ hipError_t launch_rotary(const RotaryArgs& a, bool use_bf16, hipStream_t s);
 hipError_t launch_cell_positions(const int32_t* first, int n_first, const int32_t* second, int finest, const int32_t* m_ptr,
                                  int m_capacity, float* pos, hipStream_t s);
 
-// Differential attention of the rows of B <= 64 frames (cu_q) over those of the same frames (cu_k), the first kv_len[f] of
+// Differential attention of the rows of B <= 128 frames (cu_q) over those of the same frames (cu_k), the first kv_len[f] of
 // them where it is given, the kv_len[f] that key_list names (rows within the frame, from cu_k[f] on) where that is
 // given too.  Offsets that are none set *err_flag and nothing is written.  partial: room for
 // the splits' partial results (splits > 1).  Logits are scaled by scale2 in base 2.

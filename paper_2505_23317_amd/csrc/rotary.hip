@@ -142,8 +142,9 @@ hipError_t launch(const RotaryArgs& a, hipStream_t s) {
   const int heads = a.k ? 2 * a.heads : a.heads;
   const int units_q = a.heads * a.d_head / (2 * Runs<T>::kRun), units_row = heads * a.d_head / (2 * Runs<T>::kRun);
   const int rows_wg = std::max(1, kThreads / units_row), n = a.rot_dim / 2;
-  const int grid = (a.m_capacity + rows_wg - 1) / rows_wg;
-  hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), dim3(grid), dim3(kThreads), (size_t)rows_wg * n * sizeof(float2), s,
+  const int64_t grid = ((int64_t)a.m_capacity + rows_wg - 1) / rows_wg;
+  if (grid * kThreads > 0xFFFFFFFFLL) return hipErrorInvalidValue;   // more threads than a launch has
+  hipLaunchKernelGGL((rotary_kernel<T, INTERLEAVED>), dim3((unsigned)grid), dim3(kThreads), (size_t)rows_wg * n * sizeof(float2), s,
                      static_cast<const T*>(a.q), static_cast<const T*>(a.k), a.pos, a.freq, static_cast<T*>(a.q_out),
                      static_cast<T*>(a.k_out), a.q_ld, a.k_ld, a.qo_ld, a.ko_ld, a.m_capacity, a.m_ptr, a.q_scale, rows_wg,
                      units_row, units_q, a.d_head, n, a.n_axes);

@@ -200,6 +200,20 @@ def test_one_key_far_above_the_others(K):
     _run(K, 256, n, n, qkv=(q, k, v))
 
 
+@pytest.mark.parametrize("n", ([65, 300, 1025], [1500] * 4, [1500] * 8))
+@pytest.mark.parametrize("d", (256, 384))
+def test_values_and_weights_that_are_large_together(K, d, n):
+    """Base-2 logits about 60 and values of 2^90: neither the sums nor the rows may pass what 32 bits hold."""
+    import torch
+    heads, dh = T.MODELS[d], d // T.MODELS[d]
+    q, k, v = (x.clone() for x in _inputs(d, n, n, "bf16"))
+    q.view(sum(n), heads, dh)[:, :, 0], k.view(sum(n), heads, dh)[:, :, 0] = 16.0, 60.0 / 16.0
+    q.view(sum(n), heads, dh)[:, :, 1:], k.view(sum(n), heads, dh)[:, :, 1:] = 1.0, 0.0
+    k.view(sum(n), heads, dh)[:, :, 1] = torch.randint(-4, 5, (sum(n), heads), generator=torch.Generator().manual_seed(1)).cuda().bfloat16()
+    v *= 2.0 ** 90
+    _run(K, d, n, n, qkv=(q, k, v), scale=math.log(2.0), norm=False)
+
+
 def test_scale_in_the_queries(K):
     """softmax_scale 0 takes base-2 logits: the same as ln 2."""
     import torch

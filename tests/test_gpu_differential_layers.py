@@ -239,6 +239,22 @@ def test_operators_beside_the_encoder(K):
     enc.close()
 
 
+def test_tensors_of_another_gpu(K):
+    """They are refused; the context's number is changed, so that one GPU is enough."""
+    import torch
+    s = _chain(K, 256, [40, 50], "bf16")
+    s["enc"].gpu += 1
+    with pytest.raises(ValueError):
+        _call(s)
+    p = K.norm_residual_params("rms", "none", post_g=torch.ones(256, device="cuda"))
+    x = torch.zeros(3, 256, device="cuda")
+    with pytest.raises(ValueError):
+        s["enc"].norm_residual(p, x, x.bfloat16(), x)
+    s["enc"].gpu -= 1
+    _call(s)
+    s["enc"].close()
+
+
 def test_attach_refusals(K):
     import ctypes
     cfg = synth.replace(CFGS[64], B=1)
@@ -250,6 +266,9 @@ def test_attach_refusals(K):
         with pytest.raises(K.CfdetrError) as e:
             enc.attach_differential(kept, K.rotary_params(**dict(dict(rot_dim=32), **rot)), scale)
         assert e.value.status == K.CFDETR_EINVAL
+    for bad in ({"post1": diff["post1_g"]}, {"lambda": diff["lambda"][:1]}, {"gate1": diff["gate1"][:, :32]}, {"head_g": diff["head_g"][0]}):
+        with pytest.raises(ValueError):
+            enc.attach_differential(dict(diff, **bad), K.rotary_params(32))
     enc.attach_differential(diff, K.rotary_params(32))
     with pytest.raises(K.CfdetrError):
         enc.attach_differential(diff, K.rotary_params(32))
