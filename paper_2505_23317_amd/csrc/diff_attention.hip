@@ -16,20 +16,53 @@ constexpr int kTileQ = 32;      // queries of a workgroup (a lane each)
 constexpr int kMostSplits = 128;
 
 // ---- few queries, or fp32 ----------------------------------------------------------------
-// A workgroup has 32 queries of one head and frame and one of `splits` runs of its keys.  Its four wavefronts take
+// A workgroup has 32 queries of one head and frame and one run of its keys.  Its NW wavefronts take
 // units of 32 keys in turn, each with a running maximum and sum of both maps, through LDS of its own, so that
 // there is no barrier before the end: a unit's keys are asked for as soon as the logits of the unit before have been
-// taken, its values behind that unit's.  At the end the four partial results are brought to one maximum and
+// taken, its values behind that unit's.  At the end the wavefronts' results are brought to one maximum and
 // added up in LDS, one map after the other.
-// splits > 1: row, head and split leave their maxima, sums and unscaled rows in `partial`, which
-// diff_join_kernel adds up in a fixed order.
+//
+// Where the queries alone do not fill the chip, a frame's keys are cut into runs: one frame's into `splits`, several frames' into runs
+// of about one length, as many workgroups in all as there are places (run_cut: lengths and masks are known on the device
+// only).  A row of more than one run leaves the maxima, sums and unscaled rows of each in `partial`, which diff_join_kernel adds
+// up in a fixed order.  4 frames of 300 queries over 1600, 3200, 4800 and 6400 keys: 39.2 us with as many runs for every frame,
+// 35.9 with runs of one length (a third of the keys masked and one frame without any 38.5, 35.5); frames that are equally long pay 0.2 to
+// 0.9 us for it.
+__device__ __forceinline__ int runs_of(int units, float run_inv, int most) {
+  return units == 0 ? 0 : min(most, max(1, (int)ceilf(fmaf((float)units, run_inv, -1e-3f))));
+}
+// Runs of this lane's two frames (0: no keys): every lane tries a length, from a unit a wavefront on each a ninth longer, 5,600 units at last,
+// and the shortest is taken whose workgroups have places at once (one more would take as long again); one run each if none has.
+__device__ __forceinline__ void run_cut(const Frames& fr, const int (&tiles)[2], const DiffAttentionArgs& a, int waves, int (&runs)[2]) {
+  const int lane = threadIdx.x & 63;
+  int units[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int keys = fr.k[i + 1] - fr.k[i];
+    if (a.kv_len != nullptr && 2 * lane + i < a.B) keys = min(keys, a.kv_len[2 * lane + i]);
+    units[i] = (keys + kUnitKeys - 1) / kUnitKeys;
+  }
+  const float inv = __builtin_amdgcn_exp2f(-0.15f * (float)lane) * (1.0f / (float)waves);
+  int n = 0;
+  for (int f = 0; f < a.B; ++f) n += of_lane_pair(tiles, f) * runs_of(of_lane_pair(units, f), inv, a.splits);
+  const uint64_t fit = __ballot(n * a.heads <= a.places);
+  const float chosen = fit == 0 ? 0.f : __int_as_float(__builtin_amdgcn_readlane(__float_as_int(inv), __ffsll((unsigned long long)fit) - 1));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) runs[i] = runs_of(units[i], chosen, a.splits);
+}
 template <typename T, int DH>
 struct Few {
   static constexpr int W = 2 * DH;                     // columns of both keys of a head, and of its values
   static constexpr int ROWB = W * (int)sizeof(T);      // bytes of such a row
   static constexpr int UNIT = kUnitKeys * ROWB;
+  static constexpr int ROW = 2 * W + 4;                // of partial results: maxima and sums of both maps, the two rows
   static constexpr int WAVE = 2 * UNIT > 32 * W * 4 ? 2 * UNIT : 32 * W * 4;   // LDS of a wavefront: keys and values, then the rows of a map
 };
+// Where places > 0: a row's and head's number of runs, behind the partial results.
+template <typename T, int DH>
+__device__ __forceinline__ int* runs_of_items(const DiffAttentionArgs& a) {
+  return reinterpret_cast<int*>(a.partial + (size_t)a.n_q * a.heads * a.splits * Few<T, DH>::ROW);
+}
 template <typename T, int DH, bool LIST, int NW>
 __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kernel(DiffAttentionArgs a) {
   constexpr int W = Few<T, DH>::W, ROWB = Few<T, DH>::ROWB, UNIT = Few<T, DH>::UNIT, WAVE = Few<T, DH>::WAVE;
@@ -48,28 +81,45 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kern
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // The tiles of a head and run of keys, which read the same rows, next to each other, and every XCD (workgroup mod 8), with an L2 of
-  // its own, an eighth of that order of every frame: 8 frames of 300 queries over 1600 tokens, 29.5 us with the tiles over all XCDs, 24.3 so.
+  // its own, an eighth of every frame's in that order: 8 frames of 300 queries over 1600 tokens, 29.5 us with the tiles over all XCDs, 24.1 so.
   const int tiles[2] = {(fr.q[1] - fr.q[0] + kTileQ - 1) / kTileQ, (fr.q[2] - fr.q[1] + kTileQ - 1) / kTileQ};
   const int xcd = blockIdx.x & 7;
-  int before[2], count[2];   // of a frame's workgroups: those of the XCDs before, this one's
+  int runs_in[2] = {a.splits, a.splits};
+  if (a.places > 0) run_cut(fr, tiles, a, NW, runs_in);
+  int before[2], count[2];   // of a frame's workgroups: this XCD's first, and how many
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int all = tiles[i] * a.heads * a.splits;
-    before[i] = (all >> 3) * xcd + min(xcd, all & 7);
-    count[i] = (all >> 3) + (xcd < (all & 7) ? 1 : 0);
-  }
+  for (int i = 0; i < 2; ++i) xcd_share(tiles[i] * a.heads * runs_in[i], xcd + 2 * lane + i, before[i], count[i]);
   int piece = blockIdx.x >> 3;
-  const int frame = frame_of_piece(count, sum_upto(count[0] + count[1]), piece);
-  if (frame < 0) return;
-  piece += of_lane_pair(before, frame);
-  const int frame_tiles = of_lane_pair(tiles, frame);
+  const int upto = sum_upto(count[0] + count[1]);
+  int frame = frame_of_piece(count, upto, piece);
+  if (frame >= 0) {
+    piece += of_lane_pair(before, frame);
+  } else {
+    // behind them the tiles of frames that have no run (zeros), whichever XCD
+    if (a.places == 0) return;
+    const int empty[2] = {runs_in[0] == 0 ? tiles[0] * a.heads : 0, runs_in[1] == 0 ? tiles[1] * a.heads : 0};
+    piece = 8 * (piece - __builtin_amdgcn_readlane(upto, 63)) + xcd;
+    frame = frame_of_piece(empty, sum_upto(empty[0] + empty[1]), piece);
+    if (frame < 0) return;
+  }
+  const int frame_tiles = of_lane_pair(tiles, frame), runs = max(1, of_lane_pair(runs_in, frame));
   const int group = piece / frame_tiles, tile = piece - group * frame_tiles;
   const int split = group / a.heads, head = group - split * a.heads;
   const int q0 = of_frame(fr.q, frame), nq = behind_frame(fr.q, frame) - q0;
   const int k0 = of_frame(fr.k, frame), nk_all = behind_frame(fr.k, frame) - k0;
   const int nk = a.kv_len ? min(nk_all, a.kv_len[frame]) : nk_all;
-  const int units = (nk + kUnitKeys - 1) / kUnitKeys, share = (units + a.splits - 1) / a.splits;
+  const int units = (nk + kUnitKeys - 1) / kUnitKeys, share = (units + runs - 1) / runs;
   const int u_end = min(units, (split + 1) * share);
+  if (units == 0 && runs == 1) {
+    for (int p = tid; p < kTileQ * CPR; p += 64 * NW) {
+      const int q = tile * kTileQ + p / CPR;
+      if (q >= nq) return;
+      T* const to = static_cast<T*>(a.out) + (size_t)(q0 + q) * a.out_ld + head * W;
+      *reinterpret_cast<uint4*>(to + p % CPR * Elem<T>::kChunk) = make_uint4(0, 0, 0, 0);
+      if (a.places > 0 && p % CPR == 0) runs_of_items<T, DH>(a)[(size_t)(q0 + q) * a.heads + head] = 1;
+    }
+    return;
+  }
 
   const T* const kbase = static_cast<const T*>(a.k) + (size_t)k0 * a.k_ld + head * W;
   const T* const vbase = static_cast<const T*>(a.v) + (size_t)k0 * a.v_ld + head * W;
@@ -210,9 +260,11 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kern
     }
     if (m == 0) __syncthreads();
   }
-  if (a.splits > 1) {
+  const size_t item = (size_t)(q0 + q_local) * a.heads + head;
+  if (a.places > 0 && split == 0 && part == 0 && q_local < nq) runs_of_items<T, DH>(a)[item] = runs;
+  if (runs > 1) {
     if (q_local < nq) {
-      float* const to = a.partial + (((size_t)(q0 + q_local) * a.heads + head) * a.splits + split) * (2 * W + 4);
+      float* const to = a.partial + (item * a.splits + split) * Few<T, DH>::ROW;
       if (part == 0) *reinterpret_cast<float4*>(to) = make_float4(m_all[0], m_all[1], l_all[0], l_all[1]);
 #pragma unroll
       for (int m = 0; m < 2; ++m)
@@ -238,39 +290,40 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kern
     for (int e = 0; e < CE; ++e) x[e] *= r * a.head_g[part * CE + e];
   }
   if (q_local < nq) {
-    T* const to = static_cast<T*>(a.out) + (size_t)(q0 + q_local) * a.out_ld + head * W + part * CE;
-    store_columns<T, CE>(to, x);
+    store_columns<T, CE>(static_cast<T*>(a.out) + (size_t)(q0 + q_local) * a.out_ld + head * W + part * CE, x);
   }
 }
 
-// The splits' results of a row and head, by one workgroup: wavefront w adds up splits w, w + NW, .. in that order, lane l
+// The runs' results of a row and head, by one workgroup: wavefront w adds up runs w, w + NW, .. in that order, lane l
 // a quad of columns of map l / 32, and the wavefronts' sums are added in order.
 template <typename T, int DH, int NW>
 __global__ __launch_bounds__(64 * NW) void diff_join_kernel(DiffAttentionArgs a) {
   constexpr int W = 2 * DH, Q = W / 4;   // quads of a map: 32 or 16 lanes of its 32
-  constexpr int ROW = 2 * W + 4;
-  constexpr int STEPS = kMostSplits / 32;
+  constexpr int ROW = Few<T, DH>::ROW;
   __shared__ float4 s_o[NW][64];
   __shared__ float s_l[NW][64];
   const int lane = threadIdx.x & 63, map = lane >> 5, quad = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int item = blockIdx.x, row = item / a.heads, head = item - row * a.heads;
   const float* const from = a.partial + (size_t)item * a.splits * ROW;
-  // (what is read here of a row behind the last frame, or after bad offsets, is not used)
+  // (of a row behind the last frame, or after bad offsets, nothing is known: what is read here is then not used)
+  const int cut = a.places > 0 ? runs_of_items<T, DH>(a)[item] : a.splits;
+  float top[kMostSplits / 32];
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 32; ++i) top[i] = quad + 32 * i < a.splits ? from[(size_t)(quad + 32 * i) * ROW + map] : -INFINITY;
+  if (frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad || row >= a.cu_q[a.B]) return;
+  const int runs = __builtin_amdgcn_readfirstlane(cut);
+  if (runs == 1) return;   // the row is finished
   float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const int s = quad + 32 * i;
-    if (s < a.splits) m = fmaxf(m, from[(size_t)s * ROW + map]);
-  }
-  if (frames_of(a.cu_q, a.cu_k, a.B, a.n_q, a.n_k).bad || row >= a.cu_q[a.B]) return;
+  for (int i = 0; i < kMostSplits / 32; ++i) m = quad + 32 * i < runs ? fmaxf(m, top[i]) : m;
 #pragma unroll
   for (int s = 1; s < 32; s <<= 1) m = fmaxf(m, __shfl_xor(m, s));
   const float m_ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-  for (int s = wave; s < a.splits; s += NW) {
+  for (int s = wave; s < runs; s += NW) {
     const float* const p = from + (size_t)s * ROW;
     const float f = __builtin_amdgcn_exp2f(p[map] - m_ref);
     l = fmaf(p[2 + map], f, l);
@@ -362,8 +415,10 @@ hipError_t few(const DiffAttentionArgs& a, hipStream_t s) {
   constexpr int LDS = NW * Few<T, DH>::WAVE;
   static DeviceOnce once;
   if (hipError_t e = allow_lds(diff_few_kernel<T, DH, LIST, NW>, LDS, &once); e != hipSuccess) return e;
-  // (an eighth of a frame's workgroups, rounded up, for an XCD)
-  const int64_t grid = 8 * (((int64_t)a.n_q / kTileQ + a.B) * a.heads * a.splits / 8 + a.B + 1), rows = (int64_t)a.n_q * a.heads;
+  // (an eighth of a frame's workgroups, rounded up, for an XCD; run_cut leaves the tiles or no more runs than there are places, and
+  // the tiles of frames without keys)
+  const int64_t tiles = ((int64_t)a.n_q / kTileQ + a.B) * a.heads, rows = (int64_t)a.n_q * a.heads;
+  const int64_t grid = 8 * ((a.places > 0 ? tiles + a.places : tiles * a.splits) / 8 + a.B + 2);
   if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF) return hipErrorInvalidValue;
   hipLaunchKernelGGL((diff_few_kernel<T, DH, LIST, NW>), dim3((unsigned)grid), dim3(64 * NW), LDS, s, a);
   if (a.splits > 16)
@@ -395,17 +450,22 @@ hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int 
 
 void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus) {
   a.tiles = use_bf16 && (int64_t)rows_q * a.heads >= (int64_t)64 * cus;
-  a.wide = a.tiles && (int64_t)rows_q * a.heads <= (int64_t)128 * cus;   // (no more tiles than CUs)
+  const int64_t per_frame = (rows_q + a.B - 1) / a.B;
+  a.wide = a.tiles && a.B * ((per_frame + 127) / 128) * a.heads <= cus;   // (no more tiles than CUs)
   a.splits = 1;
+  a.places = 0;
   if (a.tiles) return;
-  const int64_t per_frame = (rows_q + a.B - 1) / a.B, groups = a.B * ((per_frame + kTileQ - 1) / kTileQ) * a.heads;
+  const int64_t groups = a.B * ((per_frame + kTileQ - 1) / kTileQ) * a.heads;
   const int64_t units = (rows_k / a.B + kUnitKeys - 1) / kUnitKeys;
   a.wide = use_bf16 && groups <= cus && units >= 16;
   const int waves = a.wide ? 8 : 4, places = use_bf16 && !a.wide ? 2 * cus : cus;
-  if (units <= 4 * waves) return;
-  const int64_t row = (int64_t)a.n_q * a.heads * (4 * d_head + 4) * 4;
-  const int64_t splits = std::min<int64_t>({places / std::max<int64_t>(1, groups), units / waves, (int64_t)(partial_bytes / std::max<int64_t>(1, row)), kMostSplits});
+  if (units <= 4 * waves || 2 * groups > places) return;
+  // (a row's and head's number of runs, and its runs' results)
+  const int64_t room = (int64_t)partial_bytes / std::max<int64_t>(1, (int64_t)a.n_q * a.heads) - 4;
+  int64_t splits = std::min<int64_t>(room / ((4 * d_head + 4) * 4), kMostSplits);
+  if (a.B == 1) splits = std::min({splits, places / std::max<int64_t>(1, groups), units / waves});
   a.splits = (int)std::max<int64_t>(1, splits);
+  if (a.B > 1 && a.splits > 1) a.places = places;
 }
 
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s) {

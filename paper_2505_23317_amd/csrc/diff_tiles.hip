@@ -150,8 +150,7 @@ __device__ __forceinline__ Item item_of(const Frames& fr, const int32_t* __restr
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int items = (fr.q[i + 1] - fr.q[i] + kTileQ - 1) / kTileQ * heads;
-    first[i] = (int)((int64_t)items * xcd / 8);
-    count[i] = (int)((int64_t)items * (xcd + 1) / 8) - first[i];
+    xcd_share(items, xcd + 2 * lane + i, first[i], count[i]);
     len[i] = fr.k[i + 1] - fr.k[i];
     if (kv_len != nullptr && 2 * lane + i < B) len[i] = min(len[i], kv_len[2 * lane + i]);
   }

@@ -460,12 +460,12 @@ struct DiffAttentionArgs {
   float scale2, eps;
   int heads;   // differential heads
   bool tiles, wide;  // plan_diff_attention's: 128 queries a workgroup or 32, by eight wavefronts (wide) or four
-  int splits;
+  int splits, places;  // runs that a row's keys are cut into; places > 0: at most, by workgroups that have places at once
   float* partial;
   int32_t* err_flag;
 };
 hipError_t launch_diff_attention(const DiffAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
-// Chooses the kernel and its cut for about rows_q query and rows_k key rows (the fields tiles, wide and splits; n_q, B and heads are
+// Chooses the kernel and its cut for about rows_q query and rows_k key rows (the fields tiles, wide, splits and places; n_q, B and heads are
 // set); partial_bytes: what a.partial has room for.
 void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus);
 // list, kv_len: the keys of every frame whose mask byte is not 0, for launch_diff_attention.

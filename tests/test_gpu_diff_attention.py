@@ -69,6 +69,22 @@ def test_queries_over_other_rows(K, d, nq, nk, norm):
     _run(K, d, nq, nk, norm=norm)
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("d,nq,nk", [
+    (256, [2] * 20, [i * 397 % 4100 for i in range(20)]), (64, [5, 1, 1], [9000, 1, 0]), (384, [200, 3, 0, 40], [1025, 6000, 31, 2999]),
+    (256, [600, 1, 0, 1], [3000, 0, 500, 4000]), (64, [33] * 40, [(i * 613) % 2300 for i in range(40)]), (768, [1, 1], [30_000, 100]),
+])
+def test_runs_of_ragged_frames(K, d, nq, nk, dtype):
+    """Frames whose keys are cut into runs, of one run, and without keys, in one call."""
+    _run(K, d, nq, nk, dtype)
+
+
+@pytest.mark.parametrize("heads,frames", [(12, 12), (12, 9), (2, 60)])
+def test_tiles_that_do_not_divide_by_the_xcds(K, heads, frames):
+    n = [300 + f % 3 for f in range(frames)]
+    _run(K, 32 * heads if heads == 2 else 64 * heads, n, [130 + 7 * f for f in range(frames)], heads=heads)
+
+
 @pytest.mark.parametrize("d,n", [(256, [1600, 901, 1333, 400]), (384, [2500, 37]), (768, [1100, 1, 640])])
 def test_longer_frames(K, d, n):
     _run(K, d, n, n)
