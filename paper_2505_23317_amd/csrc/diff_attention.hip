@@ -448,18 +448,28 @@ hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int 
   return hipGetLastError();
 }
 
+// Which kernel, how many wavefronts, how many runs (us on 256 CUs, bf16; heads are pairs of heads):
+// - 128 queries a workgroup from half a tile a CU on.  19,200 rows and heads of width 64 over 1600 keys 42 (32 a workgroup 58), 24,000
+//   over 700 to 1300 39 (49); below, 9,600 over 1600 34 (39), 12,000 over 1000 26 (30), 9,000 in ten frames over 1200 30 (34).
+// - 32 queries, eight wavefronts where such workgroups leave no CU two.  One frame of 700, 1000, 1600 keys, 4 heads of width 32: 10.4,
+//   12.0, 15.0 (four wavefronts 11.4, 13.8, 19.0); from 16 units of keys on, two a wavefront: below they change nothing.  More workgroups than
+//   CUs: 300 of 1600 keys 42 (34), 312 of 400 keys 17.0 (11.6).  The LDS of fp32 rows is too large for eight.
+// - Runs where there are places for two a row and more than three units a wavefront.  One query over 600 keys 12.0 (in runs
+//   13.4), over 900 13.7 (in one 15.3), over 1200 13.2 (17.1), over 2000 14.3 (22.3).
 void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus) {
-  a.tiles = use_bf16 && (int64_t)rows_q * a.heads >= (int64_t)64 * cus;
   const int64_t per_frame = (rows_q + a.B - 1) / a.B;
-  a.wide = a.tiles && a.B * ((per_frame + 127) / 128) * a.heads <= cus;   // (no more tiles than CUs)
+  auto workgroups = [&](int queries) { return a.B * ((per_frame + queries - 1) / queries) * a.heads; };
   a.splits = 1;
   a.places = 0;
-  if (a.tiles) return;
-  const int64_t groups = a.B * ((per_frame + kTileQ - 1) / kTileQ) * a.heads;
-  const int64_t units = (rows_k / a.B + kUnitKeys - 1) / kUnitKeys;
+  a.tiles = use_bf16 && (int64_t)rows_q * a.heads >= (int64_t)64 * cus;
+  if (a.tiles) {
+    a.wide = workgroups(128) <= cus;   // (see the kernel)
+    return;
+  }
+  const int64_t groups = workgroups(kTileQ), units = (rows_k / a.B + kUnitKeys - 1) / kUnitKeys;
   a.wide = use_bf16 && groups <= cus && units >= 16;
   const int waves = a.wide ? 8 : 4, places = use_bf16 && !a.wide ? 2 * cus : cus;
-  if (units <= 4 * waves || 2 * groups > places) return;
+  if (units <= 3 * waves || 2 * groups > places) return;
   // (a row's and head's number of runs, and its runs' results)
   const int64_t room = (int64_t)partial_bytes / std::max<int64_t>(1, (int64_t)a.n_q * a.heads) - 4;
   int64_t splits = std::min<int64_t>(room / ((4 * d_head + 4) * 4), kMostSplits);

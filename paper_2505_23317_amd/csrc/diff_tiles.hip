@@ -7,7 +7,7 @@
 // Stage u: on the matrix unit the values of unit u - 1 under both maps (16 products at head width 64) and then the
 // logits of unit u + 1 (8), between them the exponentials of unit u, in an order that the compiler is not to change.
 //
-// What bounds it is a SIMD's issue: per stage and wavefront 24 products of 32 clocks' pipe and 1024 exponentials, sums and
+// What bounds it is a SIMD's issue: per stage and wavefront 24 products of 32 clocks' pipe and 2048 exponentials, sums and
 // roundings, which two wavefronts overlap.  Two logits and twice the values make 12 d_head operations a key, query and head: 8 frames of
 // 6400 tokens, 3 heads of width 64, are 7.5e11 of them in 690 us, 1.09e15 a second, where a large product of matrices
 // reaches 1.2e15.
@@ -15,7 +15,7 @@
 // KG = 1: four wavefronts, two workgroups a CU.  KG = 2: eight, where those leave CUs with one workgroup: the even
 // and the odd units of keys of the same queries, whose sums and rows (they have the same reference) are added at the end.
 // us, KG 1 / 2, heads of width 64, frames of 6784 tokens, 159 tiles: 155 / 137; 228 tiles of 9728 tokens 230 / 213; 255 of 10,880 271 / 256;
-// 270 (more than CUs) 404 / 471; 348 551 / 604; 4 frames, 96 tiles 26 / 26 (a tile of 32 queries there), 252 80.7 / 75.4, 300 125 / 145.
+// 270 (more than CUs) 404 / 471; 348 551 / 604; 4 frames, 252 tiles 80.7 / 75.4, 300 125 / 145; 12 frames of 300 queries over 3000, 216 tiles 89 / 82.
 //
 // Values lie in memory row by row.  The second product wants, for a lane's column, eight consecutive keys:
 // the transposing LDS read gives four a lane, so no copy of the values by columns is made.
