@@ -79,6 +79,16 @@ def test_runs_of_ragged_frames(K, d, nq, nk, dtype):
     _run(K, d, nq, nk, dtype)
 
 
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("d,nq,nk", [(768, [1], [9001]), (256, [40], [5000]), (384, [33, 2], [4000, 3001]), (256, [40, 1], [5000, 3])])
+def test_long_frames_without_a_key_left(K, d, nq, nk, dtype):
+    import torch
+    mask = torch.zeros(sum(nk), dtype=torch.uint8, device="cuda")
+    assert not _run(K, d, nq, nk, dtype, mask=mask).any()
+    mask[sum(nk) - 1] = 1
+    assert _run(K, d, nq, nk, dtype, mask=mask)[-1].any()
+
+
 @pytest.mark.parametrize("heads,frames", [(12, 12), (12, 9), (2, 60)])
 def test_tiles_that_do_not_divide_by_the_xcds(K, heads, frames):
     n = [300 + f % 3 for f in range(frames)]
