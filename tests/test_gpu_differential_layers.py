@@ -193,6 +193,39 @@ def test_captured_and_replayed(K, d, lengths, masked):
     s["enc"].close()
 
 
+def test_two_graphs_of_one_context(K):
+    """They share its work space (partial results, key lists): replayed in turn, with another mask and other runs each."""
+    import torch
+    pool = T.encoder(256, 9000, 3)
+    states, graphs, wants = [], [], []
+    for nq, nk, share in (([3, 1, 2], [4000, 1500, 3500], 0.4), ([40, 0, 5], [600, 2100, 5000], 0.8)):
+        g = torch.Generator(device="cuda").manual_seed(sum(nq))
+        s = dict(q=T.normal(5, sum(nq), 256).bfloat16(), kv=T.normal(6, sum(nk), 512).bfloat16(), cu_q=T.offsets(nq), cu_k=T.offsets(nk),
+                 lam=torch.full((4,), 0.4, device="cuda"), mask=(torch.rand(sum(nk), device="cuda", generator=g) > share).to(torch.uint8),
+                 out=torch.empty(sum(nq), 256, device="cuda").bfloat16())
+
+        def call(s=s):
+            pool.diff_attention(s["q"], s["kv"][:, :256], s["kv"][:, 256:], s["cu_q"], s["cu_k"], s["lam"], s["out"], key_mask=s["mask"])
+
+        call()
+        torch.cuda.synchronize()
+        wants.append(s["out"].clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        states.append(s)
+        graphs.append(graph)
+    for i in range(6):
+        for j in (0, 1) if i % 2 else (1, 0):
+            states[j]["out"].zero_()
+            graphs[j].replay()
+        torch.cuda.synchronize()
+        for s, w in zip(states, wants):
+            assert torch.equal(s["out"], w)
+    pool.sync_status()
+    pool.close()
+
+
 def test_another_stream(K):
     """The calls go to the current stream, behind what it holds."""
     import torch
