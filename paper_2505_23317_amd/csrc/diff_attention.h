@@ -195,10 +195,11 @@ __device__ __forceinline__ void unit_weights(f32x16 (&s)[2], int left, float sca
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, s[m][r]);
     top = half_max(top) * scale2;
-    if (__any(top > m_run[m] + kSlack)) {
-      const float m_new = fmaxf(m_run[m], top);
-      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[m] - m_new);
-      m_run[m] = m_new;
+    const bool follow = top > m_run[m] + kSlack;
+    if (__any(follow)) {
+      // (a query alone: what the wavefront's others are does not show in its row)
+      const float alpha = follow ? __builtin_amdgcn_exp2f(m_run[m] - top) : 1.0f;
+      if (follow) m_run[m] = top;
       l_run[m] *= alpha;
 #pragma unroll
       for (int i = 0; i < MO; ++i)

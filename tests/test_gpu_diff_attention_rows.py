@@ -1,0 +1,47 @@
+"""A row of the differential attention belongs to its query alone: the bits of one do not change with the queries beside it."""
+import pytest
+
+import differential_reference as T
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def K():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2505_23317_amd import cfdetr
+    cfdetr.load_library()
+    return cfdetr
+
+
+@pytest.mark.parametrize("d,nq,nk,dtype,level", [
+    (256, [40, 7], [2000, 333], "bf16", 0.0), (384, [33], [1500], "bf16", 0.0), (64, [50, 3], [700, 65], "f32", 0.0),
+    (384, [20], [900], "f32", 0.0), (256, [1500] * 4, [1500] * 4, "bf16", 400.0), (384, [3000] * 4, [700] * 4, "bf16", 400.0),
+])
+def test_neighbours_do_not_show(K, d, nq, nk, dtype, level):
+    """Every other query is replaced by one whose logits spread over hundreds, so that their largest one moves in many units.
+    `level`: about what all logits of the others are before the scale; 400 (144 in powers of two) is past what the kernel of many queries holds
+    without a running maximum."""
+    import torch
+    heads, dh = T.MODELS[d], d // T.MODELS[d]
+    q = T.normal(1, sum(nq), d, std=1.5)
+    k, v = T.normal(2, sum(nk), d, std=1.5), T.normal(3, sum(nk), d)
+    q.view(-1, heads, dh)[:, :, 0], k.view(-1, heads, dh)[:, :, 0] = level / 8.0, 8.0
+    q, k, v = (x.to(T.act(dtype)) for x in (q, k, v))
+    lam = torch.full((heads // 2,), 0.5, device="cuda")
+    enc = T.encoder(d, max(sum(nq), sum(nk)), len(nq), dtype)
+    outs = []
+    for steep in (False, True):
+        x = q.clone()
+        if steep:
+            x[::2] = 40 * T.normal(4, len(x[::2]), d, std=1.5).to(T.act(dtype))
+        out = torch.empty_like(q)
+        enc.diff_attention(x, k, v, T.offsets(nq), T.offsets(nk), lam, out, softmax_scale=0.25)
+        enc.sync_status()
+        outs.append(out[1::2])
+    assert torch.isfinite(outs[0]).all()
+    differ = int((outs[0] != outs[1]).any(1).sum())
+    assert torch.equal(*outs), f"{differ} of {len(outs[0])} rows differ"
+    enc.close()
