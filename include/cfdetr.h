@@ -565,6 +565,8 @@ typedef struct {
  * of the finest level, whatever its level; the position of the embedding stays.  n_heads must
  * be even (else CFDETR_ESHAPE).  The structure is copied, the weights must outlive the context, some
  * more work space is allocated.  A context is attached to once.  cfdetr_decode is as before.
+ * A frame's rows are the same bits alone or in a batch, from one call or from three, padded or not, and after
+ * any earlier run.
  */
 CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdetr_differential_weights* w);
 

@@ -450,9 +450,13 @@ cfdetr_status run_differential(cfdetr_ctx* ctx, int nseq, const RunShape& shape,
   aa.scale2 = 1.0f;   // in the rotation
   aa.eps = c.ln_eps;
   aa.heads = c.n_heads / 2;
-  const int rows = m_hint > 0 ? m_hint : m_cap;
-  plan_diff_attention(aa, rows, rows, dh, bf, partial_bytes(ctx), ctx->cus);
-  aa.partial = static_cast<float*>(ctx->h);
+  // One form for every run (bf16: 128 queries a workgroup by four wavefronts; fp32: 32), whatever its rows: the forms add a
+  // query's keys up in other orders, and a frame's rows must not show the frame's batch, the call, padding or an earlier
+  // run.  With the form chosen for the rows / with one, us: merged pass of one camera 299 / 335, of six 485 / 488, of one
+  // high-resolution frame 2,357 / 2,553 (its coarse pass 735 / 954), of four 5,350 / 5,410, of twelve three-level frames
+  // 3,770 / 3,770.  (By eight wavefronts in all of them: 336, 482, 2,356 and 915, 5,780, 4,230.)
+  aa.tiles = bf;
+  aa.splits = 1;
   aa.err_flag = ctx->err_flag;
 
   NormResidualArgs na{};
