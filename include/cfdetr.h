@@ -489,8 +489,8 @@ CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_para
  * softmax_scale q k^T of the two, a row is (A_1 - lambda[h] A_2) v, and with head_g
  * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.  The two maps'
  * products with v are taken apart: a v that is not finite leaves NaN in its column of the frame's
- * rows (lambda[h] = 0: what the first map makes of it).  Sums are 32-bit: the elements of v are
- * taken to be below 2^96 in size, with head_g below 2^60.
+ * rows.  With lambda[h] = 0 a row is what the first map makes of it, whatever the second map holds.
+ * Sums are 32-bit: the elements of v are taken to be below 2^96 in size, with head_g below 2^60.
  *   q [n_q, ld], k and v [n_k, ld] act; n_q, n_k <= max_tokens_total (else CFDETR_ECAPACITY)
  *   cu_q, cu_k  [B+1] int32 device: offsets of the frames' rows, from 0; frames may be empty.
  *               Negative lengths, or an end beyond n_q or n_k, make the call write nothing, and

@@ -274,12 +274,13 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kern
     }
     return;
   }
-  const float i0 = l_all[0] != 0.f ? 1.0f / l_all[0] : 0.f, i1 = l_all[1] != 0.f ? a.lambda[head] / l_all[1] : 0.f;
+  const float lambda = a.lambda[head];
+  const float i0 = l_all[0] != 0.f ? 1.0f / l_all[0] : 0.f, i1 = l_all[1] != 0.f ? lambda / l_all[1] : 0.f;
   float x[CE], sq = 0.f;
 #pragma unroll
   for (int e = 0; e < CE; ++e) {
     x[e] = o[0][e] * i0;
-    if (i1 != 0.f) x[e] = fmaf(-o[1][e], i1, x[e]);   // (lambda 0 leaves the first map alone, also where a value is infinite)
+    if (lambda != 0.f) x[e] = fmaf(-o[1][e], i1, x[e]);   // (lambda 0 leaves the first map alone, whatever the second holds)
     sq = fmaf(x[e], x[e], sq);
   }
   if (a.head_g) {
@@ -342,8 +343,8 @@ __global__ __launch_bounds__(64 * NW) void diff_join_kernel(DiffAttentionArgs a)
     o = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
     l += s_l[w][lane];
   }
-  const float i = l != 0.f ? (map ? -a.lambda[head] : 1.0f) / l : 0.f;
-  o = i != 0.f ? make_float4(o.x * i, o.y * i, o.z * i, o.w * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+  const float weight = map ? -a.lambda[head] : 1.0f, i = l != 0.f ? weight / l : 0.f;
+  o = weight != 0.f ? make_float4(o.x * i, o.y * i, o.z * i, o.w * i) : make_float4(0.f, 0.f, 0.f, 0.f);
   o = make_float4(half_sum(o.x), half_sum(o.y), half_sum(o.z), half_sum(o.w));
   if (a.head_g) {
     float sq = fmaf(o.x, o.x, o.y * o.y) + fmaf(o.z, o.z, o.w * o.w);

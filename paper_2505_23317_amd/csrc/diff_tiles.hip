@@ -54,7 +54,7 @@ __device__ __forceinline__ bool finish_rows(const f32x16 (&acc)[2][DH / 16], con
   for (int i = 0; i < MO; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      // (lambda 0 leaves the first map alone, also where a value is infinite)
+      // (lambda 0 leaves the first map alone, whatever the second holds)
       o[i][r] = acc[0][i][r] * i0;
       if (lambda != 0.f) o[i][r] = fmaf(-acc[1][i][r], i1, o[i][r]);
       sq = fmaf(o[i][r], o[i][r], sq);

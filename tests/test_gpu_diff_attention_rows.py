@@ -45,3 +45,38 @@ def test_neighbours_do_not_show(K, d, nq, nk, dtype, level):
     differ = int((outs[0] != outs[1]).any(1).sum())
     assert torch.equal(*outs), f"{differ} of {len(outs[0])} rows differ"
     enc.close()
+
+
+@pytest.mark.parametrize("norm", (False, True))
+@pytest.mark.parametrize("d,nq,nk,dtype", [
+    (256, [40, 7], [300, 33], "bf16"), (64, [5, 2], [70, 33], "f32"),                    # in one run
+    (384, [1], [9000], "bf16"), (64, [3], [6000], "f32"), (256, [3, 2], [4000, 900], "bf16"),   # in several, joined
+    (256, [3000] * 2, [300, 77], "bf16"), (384, [6000] * 2, [300, 77], "bf16"),          # many queries
+])
+def test_lambda_zero_leaves_the_first_map(K, d, nq, nk, dtype, norm):
+    """Keys and a query that are no numbers in the second map only: nothing of it is in the rows of a head whose lambda is 0, and
+    everything is lost in those of the head that has another."""
+    import math
+    import torch
+    heads, dh = T.MODELS[d], d // T.MODELS[d]
+    q, k, v = T.normal(1, sum(nq), d), T.normal(2, sum(nk), d), T.normal(3, sum(nk), d)
+    for h in range(heads // 2):
+        second = slice((2 * h + 1) * dh, (2 * h + 2) * dh)
+        k[3, second], k[20, second], k[nk[0] - 1, second] = math.nan, math.inf, -math.inf
+        q[0, second] = math.nan
+    q, k, v = (x.to(T.act(dtype)) for x in (q, k, v))
+    lam = torch.zeros(heads // 2, device="cuda")
+    lam[1:] = 0.5
+    g = torch.ones(2 * dh, device="cuda") if norm else None
+    out = torch.empty_like(q)
+    enc = T.encoder(d, max(sum(nq), sum(nk)), len(nq), dtype)
+    enc.diff_attention(q, k, v, T.offsets(nq), T.offsets(nk), lam, out, g)
+    enc.sync_status()
+    first = [x.clone() for x in (q, k)]
+    for x in first:
+        x[:, dh:2 * dh] = 0
+    want, bound = T.diff_attention(*(x[:, :2 * dh] for x in first), v[:, :2 * dh], nq, nk, 2, lam[:1], g, dtype)
+    T.within(out[:, :2 * dh], want, bound, f"{d} {nq} {nk}")
+    if heads > 2:
+        assert torch.isnan(out[:nq[0], 2 * dh:]).all() and torch.isfinite(out[nq[0]:, 2 * dh:]).all()
+    enc.close()
