@@ -408,7 +408,7 @@ def norm_residual_params(post="none", pre="none", post_g=None, post_b=None, pre_
             setattr(p, name, t.data_ptr())
     p.B = int(cu_seqlens.shape[0]) - 1 if cu_seqlens is not None else 0
     p.res_scale = res_scale
-    p.width = 0   # columns that Encoder.norm_residual has found the tensors to have
+    p.checked = None   # columns and GPU that Encoder.norm_residual has found the tensors to have
     return p
 
 
@@ -682,13 +682,13 @@ class Encoder:
     def norm_residual(self, params: CfdetrNormResidualParams, x, block, x_out, normed=None):
         """x, x_out: float32 [M, d]; block, normed: [M, d] in act_dtype, contiguous."""
         M, d, act = x.shape[0], self.cfg.d, "bfloat16" if self.act_bf16 else "float32"
-        if params.width != d:
+        if params.checked != (d, self.gpu):
             for name, t in params.tensors.items():
                 if t is not None and name != "cu_seqlens" and t.numel() != (params.B * d if name == "gate" and params.B else d):
                     raise ValueError(f"{name}: {d} columns expected, and a row for every frame of cu_seqlens in the gate")
                 if t is not None and t.get_device() != self.gpu:
                     raise ValueError(f"{name}: not on the context's GPU")
-            params.width = d
+            params.checked = (d, self.gpu)
         shape = (M, d)
         _expect(x, "float32", "x", shape, self.gpu)
         _expect(block, act, "block", shape, self.gpu)
