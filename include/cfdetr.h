@@ -490,7 +490,8 @@ CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_para
  * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.  The two maps'
  * products with v are taken apart: a v that is not finite leaves NaN in its column of the frame's
  * rows.  With lambda[h] = 0 a row is what the first map makes of it, whatever the second map holds.
- * Sums are 32-bit: the elements of v are taken to be below 2^96 in size, with head_g below 2^60.
+ * Sums are 32-bit, of weights of up to 2^16: the elements of v are taken to be below 2^110 / n in size for
+ * n keys of a frame, and (1 + |lambda[h]|) times them, where there is a head_g, below 2^60.
  *   q [n_q, ld], k and v [n_k, ld] act; n_q, n_k <= max_tokens_total (else CFDETR_ECAPACITY)
  *   cu_q, cu_k  [B+1] int32 device: offsets of the frames' rows, from 0; frames may be empty.
  *               Negative lengths, or an end beyond n_q or n_k, make the call write nothing, and

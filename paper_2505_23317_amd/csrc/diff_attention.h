@@ -178,6 +178,8 @@ __device__ __forceinline__ void unit_logits(const unsigned char* sK, const uint4
 // The reference of the weights follows the largest logit only once that is kSlack ahead (2^kSlack times the
 // others): a quotient is the same for any reference, and with 32 queries in a wavefront some largest logit moves in almost every
 // unit, which costs two operations for every sum (4 frames of 300 queries over 1600 to 6400 tokens: 43 -> 41.7 us).
+// A weight is then 2^kSlack at most, and a sum of n values under them n 2^kSlack |v|: 32 bits hold it as long as n |v| stays
+// below 2^(127 - kSlack), half a step of 2^-8 for the weights' rounding included.  The header promises 2^110.
 constexpr float kSlack = 16.f;
 template <typename T, int MO>
 __device__ __forceinline__ void unit_weights(f32x16 (&s)[2], int left, float scale2, float (&m_run)[2], float (&l_run)[2], f32x16 (&acc)[2][MO]) {

@@ -80,3 +80,29 @@ def test_lambda_zero_leaves_the_first_map(K, d, nq, nk, dtype, norm):
     if heads > 2:
         assert torch.isnan(out[:nq[0], 2 * dh:]).all() and torch.isfinite(out[nq[0]:, 2 * dh:]).all()
     enc.close()
+
+
+@pytest.mark.parametrize("nq,dtype,level", [(4200, "bf16", 0.0), (4200, "f32", 0.0), (16_400, "bf16", 200.0), (1, "bf16", 0.0)])
+def test_sums_at_the_limit_of_values_and_keys(K, nq, dtype, level):
+    """Values times keys just below 2^110, and nearly every logit 15.75 above those of the first keys, which is as far as the
+    reference of the weights lags: sums of 2^125.  Every value is the same c, so a row is (1 - lambda) c: the weights of either
+    map are summed twice, in the row and in the divisor, each n roundings of 2^-24 at most and in bf16 half a step of each weight."""
+    import math
+    import torch
+    nk, c = 70_001, 1.4375 * 2.0 ** 93
+    assert 0.5 < nk * c / 2.0 ** 110 < 1.0
+    q, k, v = (torch.zeros(n, 64, device="cuda") for n in (nq, nk, nk))
+    for first in (0, 32):
+        q[:, first:first + 2] = 1.0
+        k[:, first], k[256:, first + 1] = level, 15.75
+    v[:] = c
+    out = torch.empty(nq, 64, device="cuda").to(T.act(dtype))
+    enc = T.encoder(64, nk, 1, dtype)
+    q, k, v = (x.to(T.act(dtype)) for x in (q, k, v))
+    enc.diff_attention(q, k, v, T.offsets([nq]), T.offsets([nk]), torch.full((1,), 0.25, device="cuda"), out, softmax_scale=math.log(2.0))
+    enc.sync_status()
+    u = T.HALF_STEP["bf16"] if dtype == "bf16" else 0.0
+    assert torch.isfinite(out).all()
+    off = (out.double() - 0.75 * c).abs().max().item()
+    assert off <= 1.25 * (u + 2 * nk * T.EPS32) * c + T.HALF_STEP[dtype] * c, off / c
+    enc.close()
