@@ -488,8 +488,11 @@ CFDETR_API cfdetr_status cfdetr_rotary(cfdetr_ctx* ctx, const cfdetr_rotary_para
  * that lie in the columns of both.  With A_1 and A_2 the softmax over the frame's keys of
  * softmax_scale q k^T of the two, a row is (A_1 - lambda[h] A_2) v, and with head_g
  * its root-mean-square norm: divided by sqrt(mean of squares + eps), times head_g.  The two maps'
- * products with v are taken apart: a v that is not finite leaves NaN in its column of the frame's
- * rows.  With lambda[h] = 0 a row is what the first map makes of it, whatever the second map holds.
+ * products with v are taken apart.  In bf16 the weights of either are rounded to bf16 for it (half a
+ * step of 2^-8 each), so a row is off relative to those products and not to their difference: by 0.002
+ * of its size where the maps have little in common, by 0.02 where lambda = 0.9 and the second map's
+ * queries and keys are the first's plus 2 % of noise.  A v that is not finite leaves NaN in its column
+ * of the frame's rows.  With lambda[h] = 0 a row is what the first map makes of it, whatever the second map holds.
  * Sums are 32-bit, of weights of up to 2^16: the elements of v are taken to be below 2^110 / n in size for
  * n keys of a frame, and (1 + |lambda[h]|) times them, where there is a head_g, below 2^60.
  *   q [n_q, ld], k and v [n_k, ld] act; n_q, n_k <= max_tokens_total (else CFDETR_ECAPACITY)

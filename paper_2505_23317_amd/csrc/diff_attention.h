@@ -223,7 +223,8 @@ __device__ __forceinline__ void unit_rows(const unsigned char* sV, const f32x16 
   constexpr int ROWB = 2 * DH * (int)sizeof(T), MO = DH / 16;
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   if constexpr (std::is_same_v<T, bf16_t>) {
-    // A rounding of the weights to bf16: half a step of 2^-8 each, independent between keys.
+    // A rounding of the weights to bf16: half a step of 2^-8 each, independent between keys and maps (what it does to their
+    // difference: diff_tiles.hip).
     typedef __attribute__((ext_vector_type(4))) short s16x4;
     typedef __attribute__((address_space(3))) s16x4* lds4;
 #pragma unroll

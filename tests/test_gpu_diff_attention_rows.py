@@ -106,3 +106,31 @@ def test_sums_at_the_limit_of_values_and_keys(K, nq, dtype, level):
     off = (out.double() - 0.75 * c).abs().max().item()
     assert off <= 1.25 * (u + 2 * nk * T.EPS32) * c + T.HALF_STEP[dtype] * c, off / c
     enc.close()
+
+
+@pytest.mark.parametrize("norm", (False, True))
+@pytest.mark.parametrize("noise", (0.07, 0.02))
+@pytest.mark.parametrize("d,nq,nk,dtype", [
+    (384, [300], [1600], "bf16"), (384, [1], [9000], "bf16"), (256, [3000, 2500], [1600, 333], "bf16"), (384, [6000], [1600], "bf16"),
+    (384, [40], [1600], "f32"),
+])
+def test_maps_that_are_nearly_alike(K, d, nq, nk, dtype, noise, norm):
+    """The second map's queries and keys are the first's and a little noise, lambda is 0.9: the maps' products with the values are
+    many times their difference.  The bound counts the rounding of the weights relative to the products."""
+    import torch
+    heads, dh = T.MODELS[d], d // T.MODELS[d]
+    q, k, v = T.normal(1, sum(nq), d), T.normal(2, sum(nk), d), T.normal(3, sum(nk), d)
+    for x, seed in ((q, 4), (k, 5)):
+        maps = x.view(len(x), heads // 2, 2, dh)
+        maps[:, :, 1] = maps[:, :, 0] + noise * T.normal(seed, len(x), heads // 2, dh)
+    q, k, v = (x.to(T.act(dtype)) for x in (q, k, v))
+    lam, g = torch.full((heads // 2,), 0.9, device="cuda"), torch.ones(2 * dh, device="cuda") if norm else None
+    out = torch.empty_like(q)
+    enc = T.encoder(d, max(sum(nq), sum(nk)), len(nq), dtype)
+    enc.diff_attention(q, k, v, T.offsets(nq), T.offsets(nk), lam, out, g)
+    enc.sync_status()
+    want, bound = T.diff_attention(q, k, v, nq, nk, heads, lam, g, dtype)
+    worst = T.within(out, want, bound, f"{d} {nq} {nk}")
+    off = (out.double() - want).square().mean().sqrt() / want.square().mean().sqrt()
+    print(f"{dtype}, noise {noise}: off by {off.item():.2e} of the rows' size, {worst:.3f} of the bound", flush=True)
+    enc.close()
