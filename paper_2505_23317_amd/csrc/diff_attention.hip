@@ -19,7 +19,9 @@ constexpr int kMostSplits = 128;
 // A workgroup has 32 queries of one head and frame and one run of its keys.  Its NW wavefronts take
 // units of 32 keys in turn, each with a running maximum and sum of both maps, through LDS of its own, so that
 // there is no barrier before the end: a unit's keys are asked for as soon as the logits of the unit before have been
-// taken, its values behind that unit's.  At the end the wavefronts' results are brought to one maximum and
+// taken, its values behind that unit's.  (The compiler does not count the loads into LDS and believes the query's operands,
+// ordinary loads first used inside the loop, to be on their way there: the last product of a unit's logits waits for all
+// loads, the unit's values among them, before a weight is worked out.)  At the end the wavefronts' results are brought to one maximum and
 // added up in LDS, one map after the other.
 //
 // Where the queries alone do not fill the chip, a frame's keys are cut into runs: one frame's into `splits`, several frames' into runs
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) void diff_few_kern
   for (; u < u_end; u += NW) {
     const bool more = u + NW < u_end;
     const int left = nk - u * kUnitKeys, rows = listed;
-    // (the keys; their values, asked for behind them, may still be on their way)
+    // (the keys; their values, asked for behind them, need not be there yet)
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
     f32x16 s[2];
     unit_logits<T, DH>(sK, qf, s);
@@ -365,7 +367,9 @@ __global__ __launch_bounds__(64 * NW) void diff_join_kernel(DiffAttentionArgs a)
 
 // ---- masked keys ---------------------------------------------------------------------------
 // The keys of every frame that its mask leaves, in order, as row numbers within the frame, and their count: masked
-// rows are then never read.  A workgroup lists kListKeys keys of one frame, after it has counted those before.
+// rows are then never read.  A workgroup lists kListKeys keys of one frame, after it has counted those before, byte by
+// byte: the last one of a frame of 50,001 keys counts 48,000 (one query over them, 12 heads of width 64: 33.9 us without a mask, 43.5
+// with a tenth masked).
 constexpr int kListKeys = 2048;
 __global__ __launch_bounds__(kThreads) void key_list_kernel(const uint8_t* __restrict__ mask, const int32_t* __restrict__ cu_k,
                                                             int B, int n_k, int32_t* __restrict__ list, int32_t* __restrict__ kv_len) {
@@ -452,11 +456,14 @@ hipError_t launch_key_list(const uint8_t* mask, const int32_t* cu_k, int B, int 
 // Which kernel, how many wavefronts, how many runs (us on 256 CUs, bf16; heads are pairs of heads):
 // - 128 queries a workgroup from half a tile a CU on.  19,200 rows and heads of width 64 over 1600 keys 42 (32 a workgroup 58), 24,000
 //   over 700 to 1300 39 (49); below, 9,600 over 1600 34 (39), 12,000 over 1000 26 (30), 9,000 in ten frames over 1200 30 (34).
+//   The rule counts rows and not workgroups, and is wrong where frames fill little of a tile of 128: 64 frames of 42 queries
+//   (6 heads of width 64, 16,128 rows) over themselves 16.8 by 32, of 43 (16,512) 30.9 by 128; over 300 keys 28.7 and 39.1.
 // - 32 queries, eight wavefronts where such workgroups leave no CU two.  One frame of 700, 1000, 1600 keys, 4 heads of width 32: 10.4,
 //   12.0, 15.0 (four wavefronts 11.4, 13.8, 19.0); from 16 units of keys on, two a wavefront: below they change nothing.  More workgroups than
 //   CUs: 300 of 1600 keys 42 (34), 312 of 400 keys 17.0 (11.6).  The LDS of fp32 rows is too large for eight.
 // - Runs where there are places for two a row and more than three units a wavefront.  One query over 600 keys 12.0 (in runs
-//   13.4), over 900 13.7 (in one 15.3), over 1200 13.2 (17.1), over 2000 14.3 (22.3).
+//   13.4), over 900 13.7 (in one 15.3), over 1200 13.2 (17.1), over 2000 14.3 (22.3).  The mean of the frames decides: 12 queries of
+//   as many frames, 11 of 100 keys and one of 6,000, are not cut and take 49; with 600 keys each 12.8, the long one alone 14.6.
 void plan_diff_attention(DiffAttentionArgs& a, int rows_q, int rows_k, int d_head, bool use_bf16, uint64_t partial_bytes, int cus) {
   const int64_t per_frame = (rows_q + a.B - 1) / a.B;
   auto workgroups = [&](int queries) { return a.B * ((per_frame + queries - 1) / queries) * a.heads; };

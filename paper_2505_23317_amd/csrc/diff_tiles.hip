@@ -3,12 +3,17 @@
 // A workgroup has 128 queries of one head and frame, a wavefront 32 of them, a query is a lane (S^T = K Q^T,
 // O^T = V^T P^T, as in attention.hip).  Both maps of a head are worked out in one pass over the keys, because their
 // values are the same: an operand of the values read from LDS feeds a product of each.  Units of 32 keys go
-// from global memory straight into LDS, two stages before they are waited for, one barrier a stage.
+// from global memory straight into LDS, two stages ahead, one barrier a stage.
 // Stage u: on the matrix unit the values of unit u - 1 under both maps (16 products at head width 64) and then the
 // logits of unit u + 1 (8), between them the exponentials of unit u, in an order that the compiler is not to change.
 //
-// What bounds it is a SIMD's issue: per stage and wavefront 24 products of 32 clocks' pipe and 2048 exponentials, sums and
-// roundings, which two wavefronts overlap.  Two logits and twice the values make 12 d_head operations a key, query and head: 8 frames of
+// What it spends its time on: per stage and wavefront 24 products of 32 clocks' pipe and 2048 exponentials, sums and
+// roundings, which two wavefronts overlap, and waits: the compiler does not count the loads into LDS and believes the
+// query's operands, ordinary loads first used inside the loop, to be on their way there.  Without a list one of the
+// loop's two stages hence waits for all loads (vmcnt 7 to 0) in front of its logits, those that it has itself just asked for
+// among them; only the other has them two stages ahead.  With a list every entry is such a load with the wait behind it, two
+// for the keys and two for the values of each stage at head width 64: 8 frames of 6400 tokens with a third masked take 740 us, without a
+// mask 700, cut to the open keys 481.  Two logits and twice the values make 12 d_head operations a key, query and head: 8 frames of
 // 6400 tokens, 3 heads of width 64, are 7.5e11 of them in 690 us, 1.09e15 a second, where a large product of matrices
 // reaches 1.2e15.
 //
@@ -26,7 +31,8 @@
 // lambda 0.9 and a second map of the first's queries and keys plus 7 and 2 % of noise (1600 keys, heads of width 64).  What
 // the rounding leaves off, as a second operand, would be 8 d_head operations more.  A sum outside
 // [2^-64, 2^100], or that is no number, and a row that is none, sends its query through a walk with a running
-// maximum (redo_rows).
+// maximum (redo_rows), and the rest of its tile with it: nothing is asked for ahead there, and 8 frames of 6400 tokens with
+// one such query a tile, or nothing but those, take 1,790 to 1,920 us where they take 700, six frames of 400 to 1600 (width 256) 105 and 29.
 #include "diff_attention.h"
 
 namespace cfdetr {
