@@ -459,7 +459,7 @@ struct DiffAttentionArgs {
   const float *lambda, *head_g;
   float scale2, eps;
   int heads;   // differential heads
-  bool tiles, wide;  // plan_diff_attention's: 128 queries a workgroup or 32, by eight wavefronts (wide) or four
+  bool tiles, wide;  // 128 queries a workgroup or 32, by eight wavefronts (wide) or four: plan_diff_attention's, or the same for all rows
   int splits, places;  // runs that a row's keys are cut into; places > 0: at most, by workgroups that have places at once
   float* partial;
   int32_t* err_flag;

@@ -123,6 +123,27 @@ def test_a_batch_gives_what_its_frames_give_alone(K, d, dtype):
     alone.close()
 
 
+@pytest.mark.parametrize("cfg_id,frames", [(3, 6), (4, 4), (5, 8)])
+def test_the_configurations_frame_by_frame(K, cfg_id, frames):
+    """With as many rows as the contractions have tiles for: first and last frame alone, the batch twice, and in three calls."""
+    import torch
+    cfg = synth.replace(synth.config(cfg_id), B=frames, layers=2)
+    wl = synth.make_workload(cfg, seed=11)
+    enc, alone = _encoder(K, cfg, "bf16"), _encoder(K, synth.replace(cfg, B=1), "bf16")
+    img, boxes = _upload(enc, *_frames(wl, 0, frames))
+    whole = _merged(enc, img, boxes)
+    cu = whole["cu_seqlens"].tolist()
+    print(f"config {cfg_id}: {cu[-1]} mixed tokens, {frames * enc.n0} coarse ones", flush=True)
+    _same(whole, _merged(enc, img, boxes), "again")
+    _same(whole, _three_calls(enc, img, boxes), "three calls")
+    for f in (0, frames - 1):
+        got = _merged(alone, *_upload(alone, *_frames(wl, f, f + 1)))
+        assert torch.equal(got["y_mixed"][:cu[f + 1] - cu[f]], whole["y_mixed"][cu[f]:cu[f + 1]]), f"frame {f}"
+        assert torch.equal(got["y_coarse"], whole["y_coarse"][f * enc.n0:(f + 1) * enc.n0]), f"frame {f}, coarse"
+    enc.close()
+    alone.close()
+
+
 @pytest.mark.parametrize("extra", (0, 37))
 @pytest.mark.parametrize("d,dtype", FORMS)
 def test_padding_does_not_show(K, d, dtype, extra):
