@@ -567,7 +567,8 @@ typedef struct {
  *   x <- res_scale x + gate2 * post2(W2 GELU(W1 LN2 x))
  * and LNf behind the last.  A token's position is the (row, column) of its cell's centre in cells
  * of the finest level, whatever its level; the position of the embedding stays.  n_heads must
- * be even (else CFDETR_ESHAPE).  The structure is copied, the weights must outlive the context, some
+ * be even (else CFDETR_ESHAPE), and the context's hidden rows (max_tokens_total and the coarse grids of
+ * max_batch frames, times d_ffn) in bf16 below 4 GiB (else CFDETR_ECAPACITY).  The structure is copied, the weights must outlive the context, some
  * more work space is allocated.  A context is attached to once.  cfdetr_decode is as before.
  * A frame's rows are the same bits alone or in a batch, from one call or from three, padded or not, and after
  * any earlier run.

@@ -1928,6 +1928,9 @@ CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdet
   if (!std::isfinite(w->res_scale)) return fail(ctx, CFDETR_EINVAL, "res_scale is not a finite number");
   if (const char* why = check_rotary(w->rotary, c.d_model / c.n_heads, true)) return fail(ctx, CFDETR_EINVAL, why);
   if (w->rotary.n_axes != 2) return fail(ctx, CFDETR_EINVAL, "cells have two coordinates");
+  // (launch_gemm addresses its rows with 32 bits)
+  if (ctx->bf16 && ctx->tok_cap * std::max(c.d_ffn, c.d_model) * 2 >= (uint64_t)1 << 32)
+    return fail(ctx, CFDETR_ECAPACITY, "the hidden rows of max_tokens_total and the coarse grids are 4 GiB or more");
   Carver cv;
   const uint64_t o_freq = cv.take(sizeof(double) * (w->rotary.rot_dim / 2)), o_pos = cv.take(ctx->tok_cap * 2 * sizeof(float));
   hipError_t e = hipMalloc(&ctx->diff_arena, cv.off);

@@ -205,3 +205,28 @@ def test_captured_and_replayed(K, d, dtype):
         _same(eager, out, f"replay with frames {i}")
     enc.sync_status()
     enc.close()
+
+
+def test_hidden_rows_that_no_product_takes_are_refused_when_attached(K):
+    """32,768 rows and 65,536 hidden columns are 4 GiB, which the contractions do not address: refused before anything is enqueued.
+    The context goes on with what it was: a coarse pass of plain layers."""
+    cfg = synth.replace(CFGS[64], B=1, layers=1, ffn=65_536)
+    weights = synth.make_weights(cfg, 4)
+    n0 = cfg.n_cells(0)
+    diff = {"lambda": np.full((1, 1), 0.5, np.float32)}
+    for tokens, fits in ((32_767 - n0, True), (32_768 - n0, False)):
+        enc = K.Encoder(cfg, weights, max_tokens_total=tokens)
+        if fits:
+            enc.attach_differential(diff, K.rotary_params(32))
+        else:
+            with pytest.raises(K.CfdetrError) as e:
+                enc.attach_differential(diff, K.rotary_params(32))
+            assert e.value.status == K.CFDETR_ECAPACITY and "hidden rows" in str(e.value)
+        img, boxes = _upload(enc, *_frames(synth.make_workload(CFGS[64], seed=3), 0, 1))
+        out = enc.alloc_outputs(1)
+        enc.coarse_encode(img, 1, out["x0_cache"], out["y_coarse"])
+        if fits:
+            enc.multilevel_batch(img, 1, *boxes, out)
+        enc.sync_status()
+        assert np.isfinite(out["y_coarse"].cpu().numpy()).all()
+        enc.close()
