@@ -464,7 +464,8 @@ typedef struct {
 CFDETR_API cfdetr_status cfdetr_rotary_frequencies(const cfdetr_rotary_params* params, double* freq);
 
 /*
- * Rotated queries and keys of M rows (M = 0 does nothing).
+ * Rotated queries and keys of M rows (M = 0 does nothing; from 2^24 on there may be more than one launch
+ * has threads for, then nothing is enqueued: CFDETR_EDEVICE).
  *   params  host; rot_dim, n_axes and interleaved are used
  *   freq    [rot_dim / 2] device, radians per unit of position (8-byte aligned), as
  *           cfdetr_rotary_frequencies gives them or of the caller's own
