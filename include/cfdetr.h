@@ -129,12 +129,14 @@ typedef enum {
   CFDETR_K_SELECT = 0, /* A2 cell tests, compaction, offsets                   */
   CFDETR_K_PLAN = 1,   /* attention work list from the sequence offsets; of the
                           decoder also the tokens in bf16; cell positions and
-                          the list of keys that a mask leaves                  */
+                          the list of keys that a mask leaves; a step of a
+                          memory of streams                                    */
   CFDETR_K_EMBED = 2,  /* patch gather + projection + position                 */
-  CFDETR_K_GATHER = 3, /* reuse of cached coarse tokens                        */
+  CFDETR_K_GATHER = 3, /* reuse of cached coarse tokens; rows into a memory      */
   CFDETR_K_LN = 4,     /* LayerNorm; norms with gate and residual              */
   CFDETR_K_QKV = 5,    /* query/key/value projection, rotary positions         */
-  CFDETR_K_ATTN = 6,   /* variable-length self-attention, differential or not  */
+  CFDETR_K_ATTN = 6,   /* variable-length self-attention, differential or not;
+                          attention over a memory                              */
   CFDETR_K_OUT = 7,    /* output projection + residual                         */
   CFDETR_K_FF1 = 8,    /* first FFN projection + GELU                          */
   CFDETR_K_FF2 = 9,    /* second FFN projection + residual; where one kernel does
@@ -575,6 +577,128 @@ typedef struct {
  * any earlier run.
  */
 CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdetr_differential_weights* w);
+
+/* ---- Memory of streams ------------------------------------------------------------------
+ *
+ * Keys and values of tokens that outlive the call that made them: those of a camera's last frames, of an object's track,
+ * of a clip.  How many tokens a stream gets is known on the device only (cu_seqlens of the selection), so
+ * the memory is cut into pages that streams take and give back there.  Everything below the sizes is the
+ * caller's memory, so that the layers of a model may have caches of their own under one state, and states may be copied:
+ *   caches      rows [n_pages * page_size, ld] of n_kv_heads * d_head act elements, keys and values; a row's number is its slot
+ *   span        [B, 2] int32 (8-byte aligned): stream b holds `held` tokens from position `first` on
+ *   table       [B, max_pages] int32: the token at position p lies in page table[b][(p / page_size) mod max_pages],
+ *               in slot page * page_size + p mod page_size.  Positions stay below 2 max_pages pages.
+ *   free_pages  [n_pages] int32, a ring of page numbers; pool [2] int32 = (where the free ones begin, how many they are)
+ * At the start no stream holds anything: span 0, free_pages 0 .. n_pages - 1, pool (0, n_pages); table may hold anything.
+ * B is the same for all calls on a state.  Rows of act and their distances as for the operators above (d <= ld is
+ * n_kv_heads * d_head <= ld for caches and key rows).  No call waits, allocates or depends on the host knowing a length: a captured one
+ * may be replayed on other contents.
+ */
+typedef struct {
+  int32_t page_size;   /* tokens of a page: a power of two, 8..1024                                */
+  int32_t n_pages;     /* >= 1; n_pages * page_size < 2^31                                          */
+  int32_t max_pages;   /* columns of a table: pages that a stream may touch at once; max_pages *
+                          page_size <= 2^29                                                         */
+  int32_t max_streams; /* 1..4096; max_streams * max_pages <= 2^28                                  */
+  int32_t n_kv_heads;  /* key heads, a divisor of n_heads: that many query heads share one          */
+} cfdetr_memory_config;
+
+/*
+ * Gives the context a memory of these sizes (else CFDETR_ESHAPE) and the work space of its operators.  Once per context.
+ */
+CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memory_config* cfg);
+
+/*
+ * One step of a state: first drop[b] tokens of every stream b are forgotten, from its oldest on (all, where it holds no
+ * more; its pages then all go back: the stream has ended), then room is made for cu_new[b+1] - cu_new[b] tokens behind the rest.
+ *   drop    [B] int32 device, >= 0; NULL: nothing is forgotten
+ *   cu_new  [B+1] int32 device: offsets of the streams' new tokens, from 0, as the selection writes them
+ *   n_new   rows of `slots`, 0..2^30; an end of cu_new beyond it is an error
+ *   span, table, pool -> span_out, table_out, pool_out: each output is its input or lies apart from all other arguments.  A table
+ *           that lies apart gets the page numbers of what the streams then hold, its other entries are left as they were; one in
+ *           place only those that change.
+ *   free_pages  in and out: pages are taken from the front of the free ones and given back behind them, in the order of
+ *           the streams; what a step gives back may be taken from the next step on
+ *   slots   [n_new] int32 out: the slot of every new token, -1 behind the last
+ * If the free pages do not suffice, a stream would touch more than max_pages pages, or an argument is none (a negative drop,
+ * offsets that descend or end beyond n_new, a span or pool that no step leaves), then nothing is forgotten or added for any stream: the outputs
+ * are the state as it was, every slot is -1, and cfdetr_sync_status reports CFDETR_ECAPACITY.
+ */
+CFDETR_API cfdetr_status cfdetr_memory_advance(cfdetr_ctx* ctx, int32_t B, const int32_t* drop, const int32_t* cu_new,
+                                    int32_t n_new, const int32_t* span, int32_t* span_out,
+                                    const int32_t* table, int32_t* table_out, const int32_t* pool,
+                                    int32_t* pool_out, int32_t* free_pages, int32_t* slots,
+                                    void* hip_stream);
+
+/*
+ * Rotary positions of up to four axes, e.g. time, row and column, with a number of pairs for each: pair i of a
+ * head is turned by pos[axis(i)] * f_i radians, as in cfdetr_rotary.
+ */
+#define CFDETR_MAX_AXES 4
+typedef struct {
+  int32_t rot_dim;      /* features of a head that are rotated, from the first on: a multiple of 16, at most d_head */
+  int32_t n_axes;       /* 1..4                                                                          */
+  int32_t pairs[CFDETR_MAX_AXES]; /* pairs of an axis, >= 1 for each; together rot_dim / 2                 */
+  int32_t in_turn;      /* 0: the pairs of axis 0, then those of axis 1, ..; 1: one of each axis in turn, an axis
+                           whose pairs are used up being passed over                                     */
+  int32_t shared_ladder;/* 0: pair j of an axis that has P has f = base^(-j / P); 1: pair i of the head's n,
+                           whatever its axis, has base^(-i / n)                                          */
+  int32_t interleaved;  /* 0: pair i = features i and i + n; 1: features 2i and 2i + 1                     */
+  double base;          /* > 1, e.g. 10000                                                               */
+} cfdetr_rotary_axes_params;
+
+/* Host only: freq and axis [rot_dim / 2] (host) = f_i and axis(i).  All fields of `params` are checked (rot_dim at most
+ * 64); cfdetr_last_error(NULL) says why it failed. */
+CFDETR_API cfdetr_status cfdetr_rotary_axes_table(const cfdetr_rotary_axes_params* params, double* freq, uint8_t* axis);
+
+/*
+ * Rotated queries and keys of M rows (M = 0 does nothing), as cfdetr_rotary.
+ *   params  host; rot_dim, n_axes and interleaved are used
+ *   freq, axis  [rot_dim / 2] device (freq 8-byte aligned), as cfdetr_rotary_axes_table gives them or of the caller's own; an axis
+ *           of n_axes or more counts as the last
+ *   pos     [M, n_axes] fp32 (4-byte aligned)
+ *   k_heads heads of a key row, 1..n_heads; k and k_out may both be NULL (k_heads is then not used)
+ *   others as for cfdetr_rotary
+ */
+CFDETR_API cfdetr_status cfdetr_rotary_axes(cfdetr_ctx* ctx, const cfdetr_rotary_axes_params* params, const double* freq,
+                                 const uint8_t* axis, const float* pos, int32_t M, const void* q,
+                                 int32_t q_ld, void* q_out, int32_t q_out_ld, float q_scale,
+                                 const void* k, int32_t k_ld, void* k_out, int32_t k_out_ld,
+                                 int32_t k_heads, void* hip_stream);
+
+/*
+ * Keys and values of M new tokens into their slots (M = 0 does nothing), the keys turned on the way.
+ *   k, v    [M, ld] act: n_kv_heads heads each
+ *   slots   [M] int32 device, as cfdetr_memory_advance writes them.  A row whose slot is negative goes nowhere; one of
+ *           n_pages * page_size or more neither, and cfdetr_sync_status reports CFDETR_ECAPACITY.  No slot may come twice (pieces of either
+ *           row would be in it).
+ *   k_cache, v_cache  out; rows of other slots are untouched.  They must not overlap k and v.
+ *   params, freq, axis, pos  as for cfdetr_rotary_axes; params NULL: the keys are written as they are and the others not used
+ */
+CFDETR_API cfdetr_status cfdetr_memory_append(cfdetr_ctx* ctx, const cfdetr_rotary_axes_params* params, const double* freq,
+                                   const uint8_t* axis, const float* pos, int32_t M, const void* k,
+                                   int32_t k_ld, const void* v, int32_t v_ld, const int32_t* slots,
+                                   void* k_cache, int32_t k_cache_ld, void* v_cache,
+                                   int32_t v_cache_ld, void* hip_stream);
+
+/*
+ * Attention of one new token of every stream over all that the stream holds (its own key and value among it, once they are appended):
+ * with G = n_heads / n_kv_heads, head h of out is softmax(softmax_scale q_h k_g^T) v_g over the held tokens, g = h / G.
+ *   q       [B, ld] act: n_heads heads
+ *   span, table  as a step leaves them.  A span that no step leaves makes the call write nothing; a page number outside 0 .. n_pages - 1
+ *           is not read (its tokens count as masked).  Both are reported by cfdetr_sync_status as CFDETR_ECAPACITY.
+ *   key_mask  [n_pages * page_size] uint8 device, by slot, 0: the token is not read, whatever it holds; NULL: all are read
+ *   softmax_scale  > 0; or 0: the queries have been multiplied by log2(e) / sqrt(d_head) already
+ *   out     [B, ld] act; may be q (with the same ld).  The row of a stream that holds no token that may be read is 0.
+ * Sums are 32-bit, of weights of up to 2^16 (the elements of v are taken to be below 2^110 / n in size for n tokens).  A v that
+ * is not finite leaves NaN in its column.  Sums over many tokens may be split over the chip; they are added in a
+ * fixed order, so the same call gives the same bits.
+ */
+CFDETR_API cfdetr_status cfdetr_memory_attention(cfdetr_ctx* ctx, const void* q, int32_t q_ld, int32_t B, const void* k_cache,
+                                      int32_t k_cache_ld, const void* v_cache, int32_t v_cache_ld,
+                                      const int32_t* span, const int32_t* table,
+                                      const uint8_t* key_mask, float softmax_scale, void* out,
+                                      int32_t out_ld, void* hip_stream);
 
 /* ------------------------------------------------------------------------
  * NPFP** scheduling decisions (Sec. IV).  Host memory only; no GPU work, no context,

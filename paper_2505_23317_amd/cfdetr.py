@@ -23,6 +23,7 @@ LIB_PATH = os.path.join(_HERE, "libcfdetr.so")
 CFDETR_OK, CFDETR_EINVAL, CFDETR_ESHAPE, CFDETR_ECAPACITY, CFDETR_ENOMEM, CFDETR_EDEVICE = range(6)
 CFDETR_BF16, CFDETR_FP32 = 0, 1
 CFDETR_MAX_LEVELS = 3
+CFDETR_MAX_AXES = 4
 KERNEL_NAMES = ["select", "plan", "embed", "gather", "layernorm", "qkv", "attention",
                 "out_proj", "ffn1", "ffn2", "roi", "dec"]
 CFDETR_K_COUNT = len(KERNEL_NAMES)
@@ -38,6 +39,8 @@ EXPORTS = [
     "cfdetr_sched_decide", "cfdetr_decoder_attach", "cfdetr_decode", "cfdetr_merge_detections",
     "cfdetr_rotary_frequencies", "cfdetr_rotary", "cfdetr_diff_attention", "cfdetr_norm_residual",
     "cfdetr_differential_attach",
+    "cfdetr_memory_attach", "cfdetr_memory_advance", "cfdetr_memory_append", "cfdetr_memory_attention",
+    "cfdetr_rotary_axes_table", "cfdetr_rotary_axes",
 ]
 POLICIES = {"C": 0, "CF": 1, "[C]F": 2, "C[F]": 3, "[C][F]": 4}
 SCHED_ACTIONS = ["idle", "coarse", "fine"]
@@ -114,6 +117,16 @@ class CfdetrDifferentialWeights(ctypes.Structure):
                 + [("res_scale", ctypes.c_float), ("rotary", CfdetrRotaryParams)])
 
 
+class CfdetrMemoryConfig(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("page_size", "n_pages", "max_pages", "max_streams", "n_kv_heads")]
+
+
+class CfdetrRotaryAxesParams(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * CFDETR_MAX_AXES),
+                ("in_turn", ctypes.c_int32), ("shared_ladder", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("base", ctypes.c_double)]
+
+
 _lib = None
 
 
@@ -187,6 +200,19 @@ def load_library() -> ctypes.CDLL:
     lib.cfdetr_norm_residual.restype = ctypes.c_int
     lib.cfdetr_differential_attach.argtypes = [vp, ctypes.POINTER(CfdetrDifferentialWeights)]
     lib.cfdetr_differential_attach.restype = ctypes.c_int
+    axes = ctypes.POINTER(CfdetrRotaryAxesParams)
+    lib.cfdetr_memory_attach.argtypes = [vp, ctypes.POINTER(CfdetrMemoryConfig)]
+    lib.cfdetr_memory_attach.restype = ctypes.c_int
+    lib.cfdetr_memory_advance.argtypes = [vp, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.cfdetr_memory_advance.restype = ctypes.c_int
+    lib.cfdetr_rotary_axes_table.argtypes = [axes, dp, ctypes.POINTER(ctypes.c_uint8)]
+    lib.cfdetr_rotary_axes_table.restype = ctypes.c_int
+    lib.cfdetr_rotary_axes.argtypes = [vp, axes, vp, vp, vp, i32, vp, i32, vp, i32, f32, vp, i32, vp, i32, i32, vp]
+    lib.cfdetr_rotary_axes.restype = ctypes.c_int
+    lib.cfdetr_memory_append.argtypes = [vp, axes, vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, i32, vp]
+    lib.cfdetr_memory_append.restype = ctypes.c_int
+    lib.cfdetr_memory_attention.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, f32, vp, i32, vp]
+    lib.cfdetr_memory_attention.restype = ctypes.c_int
     lib.cfdetr_profile_begin.argtypes = [vp]
     lib.cfdetr_profile_begin.restype = ctypes.c_int
     lib.cfdetr_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_float),
@@ -419,6 +445,53 @@ def cfdetr_norm_residual(ctx, params: CfdetrNormResidualParams, x, block, x_out,
 
 def cfdetr_differential_attach(ctx, weights: CfdetrDifferentialWeights) -> None:
     _check(load_library().cfdetr_differential_attach(ctx, ctypes.byref(weights)), ctx)
+
+
+def cfdetr_memory_attach(ctx, cfg: CfdetrMemoryConfig) -> None:
+    _check(load_library().cfdetr_memory_attach(ctx, ctypes.byref(cfg)), ctx)
+
+
+def cfdetr_memory_advance(ctx, B, drop, cu_new, n_new, span, span_out, table, table_out, pool, pool_out, free_pages,
+                          slots, stream=0) -> None:
+    _check(load_library().cfdetr_memory_advance(ctx, B, drop, cu_new, n_new, span, span_out, table, table_out, pool,
+                                                pool_out, free_pages, slots, stream), ctx)
+
+
+def rotary_axes_params(rot_dim: int, pairs, in_turn: bool = False, shared_ladder: bool = False, interleaved: bool = False,
+                       base: float = 10000.0) -> CfdetrRotaryAxesParams:
+    """pairs: how many of the rot_dim / 2 pairs each axis has."""
+    if not 1 <= len(pairs) <= CFDETR_MAX_AXES:
+        raise ValueError(f"pairs: 1 to {CFDETR_MAX_AXES} axes expected")
+    return CfdetrRotaryAxesParams(rot_dim, len(pairs), (ctypes.c_int32 * CFDETR_MAX_AXES)(*pairs), int(in_turn),
+                                  int(shared_ladder), int(interleaved), base)
+
+
+def cfdetr_rotary_axes_table(params: CfdetrRotaryAxesParams):
+    """Frequency and axis of the rot_dim / 2 pairs, as two lists (host)."""
+    # (a bad rot_dim is refused before anything is written)
+    n = max(1, params.rot_dim // 2)
+    freq, axis = (ctypes.c_double * n)(), (ctypes.c_uint8 * n)()
+    _check(load_library().cfdetr_rotary_axes_table(ctypes.byref(params), freq, axis))
+    return list(freq), list(axis)
+
+
+def cfdetr_rotary_axes(ctx, params: CfdetrRotaryAxesParams, freq, axis, pos, M, q, q_ld, q_out, q_out_ld, q_scale, k,
+                       k_ld, k_out, k_out_ld, k_heads, stream=0) -> None:
+    _check(load_library().cfdetr_rotary_axes(ctx, ctypes.byref(params), freq, axis, pos, M, q, q_ld, q_out, q_out_ld,
+                                             q_scale, k, k_ld, k_out, k_out_ld, k_heads, stream), ctx)
+
+
+def cfdetr_memory_append(ctx, params: Optional[CfdetrRotaryAxesParams], freq, axis, pos, M, k, k_ld, v, v_ld, slots,
+                         k_cache, k_cache_ld, v_cache, v_cache_ld, stream=0) -> None:
+    _check(load_library().cfdetr_memory_append(ctx, None if params is None else ctypes.byref(params), freq, axis, pos,
+                                               M, k, k_ld, v, v_ld, slots, k_cache, k_cache_ld, v_cache, v_cache_ld,
+                                               stream), ctx)
+
+
+def cfdetr_memory_attention(ctx, q, q_ld, B, k_cache, k_cache_ld, v_cache, v_cache_ld, span, table, key_mask,
+                            softmax_scale, out, out_ld, stream=0) -> None:
+    _check(load_library().cfdetr_memory_attention(ctx, q, q_ld, B, k_cache, k_cache_ld, v_cache, v_cache_ld, span,
+                                                  table, key_mask, softmax_scale, out, out_ld, stream), ctx)
 
 
 def cfdetr_profile_begin(ctx) -> None:
@@ -714,6 +787,116 @@ class Encoder:
         w.res_scale, w.rotary = res_scale, rotary
         cfdetr_differential_attach(self.ctx, w)
         self.diff_dev, self.c_diff = dev, w
+
+    # -- memory of streams -----------------------------------------------------------------
+    def attach_memory(self, page_size: int, n_pages: int, max_pages: int, max_streams: int,
+                      n_kv_heads: Optional[int] = None):
+        """n_kv_heads: key heads, a divisor of the context's heads; None for as many."""
+        mem = CfdetrMemoryConfig(page_size, n_pages, max_pages, max_streams, n_kv_heads or self.cfg.heads)
+        cfdetr_memory_attach(self.ctx, mem)
+        self.mem, self.kv_dim, self.n_slots = mem, mem.n_kv_heads * self.cfg.d_head, n_pages * page_size
+
+    def alloc_memory(self, B: int):
+        """A state of B streams that hold nothing yet, and a cache for the keys and values of one layer."""
+        import torch
+        m, dev = self._memory(), f"cuda:{self.gpu}"
+        return {
+            "span": torch.zeros((B, 2), dtype=torch.int32, device=dev),
+            "table": torch.zeros((B, m.max_pages), dtype=torch.int32, device=dev),
+            "pool": torch.tensor([0, m.n_pages], dtype=torch.int32, device=dev),
+            "free_pages": torch.arange(m.n_pages, dtype=torch.int32, device=dev),
+            "k_cache": torch.zeros((self.n_slots, self.kv_dim), dtype=self.act, device=dev),
+            "v_cache": torch.zeros((self.n_slots, self.kv_dim), dtype=self.act, device=dev),
+        }
+
+    def _memory(self) -> CfdetrMemoryConfig:
+        mem = getattr(self, "mem", None)
+        if mem is None:
+            raise ValueError("no memory attached")
+        return mem
+
+    def memory_advance(self, cu_new, span, table, pool, free_pages, slots, drop=None, span_out=None, table_out=None,
+                       pool_out=None):
+        """cu_new: int32 [B + 1]; span: int32 [B, 2]; table: int32 [B, max_pages]; pool: int32 [2]; free_pages: int32
+        [n_pages]; slots: int32 [n_new] out; drop: int32 [B] or None.  The outputs are the inputs where they are not given."""
+        m, gpu = self._memory(), self.gpu
+        B, n_new = span.shape[0], slots.shape[0]
+        _expect(cu_new, "int32", "cu_new", (B + 1,), gpu)
+        _expect(slots, "int32", "slots", (n_new,), gpu)
+        _expect(free_pages, "int32", "free_pages", (m.n_pages,), gpu)
+        if drop is not None:
+            _expect(drop, "int32", "drop", (B,), gpu)
+        both = []
+        for t, out, what, shape in ((span, span_out, "span", (B, 2)), (table, table_out, "table", (B, m.max_pages)),
+                                    (pool, pool_out, "pool", (2,))):
+            _expect(t, "int32", what, shape, gpu)
+            if out is None:
+                out = t
+            elif out is not t:
+                _expect(out, "int32", what + "_out", shape, gpu)
+            both += [t.data_ptr(), out.data_ptr()]
+        cfdetr_memory_advance(self.ctx, B, _ptr(drop), cu_new.data_ptr(), n_new, *both, free_pages.data_ptr(),
+                              slots.data_ptr(), self._stream())
+
+    def rotary_axes(self, params: CfdetrRotaryAxesParams, freq, axis, pos, q, q_out, k=None, k_out=None, q_scale=1.0):
+        """freq: float64, axis: uint8 [rot_dim / 2]; pos: float32 [M, n_axes]; q and q_out: [M, d], k and k_out: [M, key
+        heads * d_head] in act_dtype, rows may lie apart (columns of a wider tensor)."""
+        shape = (q.shape[0], self.cfg.d)
+        M = shape[0]
+        self._expect_axes(params, freq, axis, pos, M)
+        rows = self._rows
+        q_ld, qo_ld, k_ld, ko_ld, k_heads = rows(q, shape, "q"), rows(q_out, shape, "q_out"), 0, 0, 0
+        if k is not None or k_out is not None:
+            if k is None or k_out is None:
+                raise ValueError("k and k_out go together")
+            shape = (M, k.shape[1])
+            k_heads, rest = divmod(shape[1], self.cfg.d_head)
+            if rest:
+                raise ValueError("k: whole heads expected")
+            k_ld, ko_ld = rows(k, shape, "k"), rows(k_out, shape, "k_out")
+            k, k_out = k.data_ptr(), k_out.data_ptr()
+        cfdetr_rotary_axes(self.ctx, params, freq.data_ptr(), axis.data_ptr(), pos.data_ptr(), M, q.data_ptr(), q_ld,
+                           q_out.data_ptr(), qo_ld, q_scale, k, k_ld, k_out, ko_ld, k_heads, self._stream())
+
+    def _expect_axes(self, params, freq, axis, pos, M):
+        n = params.rot_dim // 2
+        _expect(freq, "float64", "freq", (n,), self.gpu)
+        _expect(axis, "uint8", "axis", (n,), self.gpu)
+        _expect(pos, "float32", "pos", (M, params.n_axes), self.gpu)
+
+    def memory_append(self, k, v, slots, k_cache, v_cache, params: Optional[CfdetrRotaryAxesParams] = None, freq=None,
+                      axis=None, pos=None):
+        """k, v: [M, n_kv_heads * d_head] in act_dtype, caches [n_pages * page_size, n_kv_heads * d_head], rows may lie apart;
+        slots: int32 [M].  params: the keys are turned by freq, axis and pos (as for rotary_axes); None: they are not."""
+        self._memory()
+        M, shape, cache, rows = k.shape[0], (k.shape[0], self.kv_dim), (self.n_slots, self.kv_dim), self._rows
+        _expect(slots, "int32", "slots", (M,), self.gpu)
+        if params is not None:
+            self._expect_axes(params, freq, axis, pos, M)
+            freq, axis, pos = freq.data_ptr(), axis.data_ptr(), pos.data_ptr()
+        elif freq is not None or axis is not None or pos is not None:
+            raise ValueError("freq, axis and pos go with params")
+        cfdetr_memory_append(self.ctx, params, freq, axis, pos, M, k.data_ptr(), rows(k, shape, "k"), v.data_ptr(),
+                             rows(v, shape, "v"), slots.data_ptr(), k_cache.data_ptr(), rows(k_cache, cache, "k_cache"),
+                             v_cache.data_ptr(), rows(v_cache, cache, "v_cache"), self._stream())
+
+    def memory_attention(self, q, k_cache, v_cache, span, table, out, key_mask=None, softmax_scale=None):
+        """q, out: [B, d]; caches [n_pages * page_size, n_kv_heads * d_head]; span: int32 [B, 2]; table: int32 [B, max_pages];
+        key_mask: uint8 [n_pages * page_size] or None.  softmax_scale: None for 1 / sqrt(d_head), 0 for queries that have
+        been multiplied by log2(e) / sqrt(d_head)."""
+        m = self._memory()
+        B, cache, rows = q.shape[0], (self.n_slots, self.kv_dim), self._rows
+        shape = (B, self.cfg.d)
+        _expect(span, "int32", "span", (B, 2), self.gpu)
+        _expect(table, "int32", "table", (B, m.max_pages), self.gpu)
+        if key_mask is not None:
+            _expect(key_mask, "uint8", "key_mask", (self.n_slots,), self.gpu)
+        if softmax_scale is None:
+            softmax_scale = self.cfg.d_head ** -0.5
+        cfdetr_memory_attention(self.ctx, q.data_ptr(), rows(q, shape, "q"), B, k_cache.data_ptr(),
+                                rows(k_cache, cache, "k_cache"), v_cache.data_ptr(), rows(v_cache, cache, "v_cache"),
+                                span.data_ptr(), table.data_ptr(), _ptr(key_mask), softmax_scale, out.data_ptr(),
+                                rows(out, shape, "out"), self._stream())
 
     def sync_status(self):
         cfdetr_sync_status(self.ctx, self._stream())

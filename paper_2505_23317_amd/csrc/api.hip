@@ -13,6 +13,7 @@
 
 #include "few_rows.h"
 #include "kernels.h"
+#include "stream_memory.h"
 
 using namespace cfdetr;
 
@@ -112,6 +113,13 @@ struct cfdetr_ctx {
   void* diff_arena = nullptr;
   double* diff_freq = nullptr;    // [rot_dim / 2]
   float* diff_pos = nullptr;      // [Tm, 2] positions of the rows of the run in flight
+
+  // memory of streams (cfdetr_memory_attach): its own allocation
+  bool has_mem = false;
+  cfdetr_memory_config mem;
+  int mem_page_bits = 0;
+  void* mem_arena = nullptr;
+  int32_t* mem_arrived = nullptr;   // counter of workgroups, 0 between calls
 
   std::string err;
 
@@ -244,11 +252,53 @@ void rotary_frequencies(const cfdetr_rotary_params& p, double* freq) {
 
 // Rows of act elements that an operator reads or writes; 32 of them are addressed with 32 bits.
 constexpr int kMaxRowElements = 1 << 24;
-const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld) {
+const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld, int columns) {
   if (!p) return "null pointer";
-  if (ld < ctx->cfg.d_model || ld > kMaxRowElements) return "rows must be d_model to 2^24 elements apart";
+  if (ld < columns || ld > kMaxRowElements) return "rows must be d_model to 2^24 elements apart";
   if (!aligned16(p) || (size_t)ld * ctx->esz % 16) return "rows must begin on multiples of 16 bytes";
   return nullptr;
+}
+const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld) { return check_rows(ctx, p, ld, ctx->cfg.d_model); }
+
+// Fields of a rotation of several axes that the kernel uses, for heads of `d_head`; with `table` also those of its table.
+const char* check_rotary_axes(const cfdetr_rotary_axes_params& p, int d_head, bool table) {
+  if (p.rot_dim < 16 || p.rot_dim % 16 || p.rot_dim > d_head) return "rot_dim must be a multiple of 16, at most the head width";
+  if (p.n_axes < 1 || p.n_axes > CFDETR_MAX_AXES) return "n_axes must be 1..4";
+  if (p.interleaved != 0 && p.interleaved != 1) return "interleaved must be 0 or 1";
+  if (!table) return nullptr;
+  int64_t all = 0;
+  for (int a = 0; a < p.n_axes; ++a) {
+    if (p.pairs[a] < 1) return "every axis must have a pair";
+    all += p.pairs[a];
+  }
+  if (all != p.rot_dim / 2) return "the axes' pairs must be rot_dim / 2 together";
+  if ((p.in_turn != 0 && p.in_turn != 1) || (p.shared_ladder != 0 && p.shared_ladder != 1)) return "in_turn and shared_ladder must be 0 or 1";
+  if (!(p.base > 1.0) || !std::isfinite(p.base)) return "base must be a number above 1";
+  return nullptr;
+}
+
+void rotary_axes_table(const cfdetr_rotary_axes_params& p, double* freq, uint8_t* axis) {
+  const int n = p.rot_dim / 2;
+  int used[CFDETR_MAX_AXES] = {}, a = 0;
+  for (int i = 0; i < n; ++i) {
+    while (used[a] == p.pairs[a]) a = (a + 1) % p.n_axes;   // (some axis has a pair left: they are n together)
+    const double part = p.shared_ladder ? (double)i / n : (double)used[a] / p.pairs[a];
+    freq[i] = std::pow(p.base, -part);
+    axis[i] = (uint8_t)a;
+    ++used[a];
+    if (p.in_turn) a = (a + 1) % p.n_axes;
+  }
+}
+
+const char* check_axes_pointers(const double* freq, const uint8_t* axis, const float* pos) {
+  if (!freq || !axis || !pos) return "null pointer";
+  if (reinterpret_cast<uintptr_t>(freq) % 8 || reinterpret_cast<uintptr_t>(pos) % 4) return "frequencies or positions are not aligned";
+  return nullptr;
+}
+bool aligned4(std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return false;
+  return true;
 }
 
 struct Carver {
@@ -294,6 +344,15 @@ cfdetr_status check_call(cfdetr_ctx* ctx, int B) {
   if (B < 1) return fail(ctx, CFDETR_EINVAL, "B must be >= 1");
   if (B > ctx->cfg.max_batch) return fail(ctx, CFDETR_ECAPACITY, "B exceeds max_batch");
   return check_device(ctx);
+}
+
+// A call on a context's memory of streams.
+cfdetr_status check_memory_call(cfdetr_ctx* ctx, int B) {
+  if (cfdetr_status st = check_device(ctx); st != CFDETR_OK) return st;
+  if (!ctx->has_mem) return fail(ctx, CFDETR_EINVAL, "no memory attached");
+  if (B < 1) return fail(ctx, CFDETR_EINVAL, "B must be >= 1");
+  if (B > ctx->mem.max_streams) return fail(ctx, CFDETR_ECAPACITY, "B exceeds max_streams");
+  return CFDETR_OK;
 }
 
 // Patch embedding of the tokens of one level into ctx->x (and optionally out2).
@@ -1422,6 +1481,7 @@ CFDETR_API void cfdetr_destroy(cfdetr_ctx* ctx) {
   if (ctx->arena) hipFree(ctx->arena);
   if (ctx->dec_arena) hipFree(ctx->dec_arena);
   if (ctx->diff_arena) hipFree(ctx->diff_arena);
+  if (ctx->mem_arena) hipFree(ctx->mem_arena);
   delete ctx;
 }
 
@@ -1951,6 +2011,199 @@ CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdet
   ctx->diff_pos = reinterpret_cast<float*>(base + o_pos);
   ctx->fw = *w;
   ctx->has_diff = true;
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memory_config* cfg) {
+  cfdetr_status st = check_device(ctx);
+  if (st != CFDETR_OK) return st;
+  if (!cfg) return fail(ctx, CFDETR_EINVAL, "null argument");
+  if (ctx->has_mem) return fail(ctx, CFDETR_EINVAL, "the context already has a memory");
+  if (const char* why = check_memory_sizes(cfg->page_size, cfg->n_pages, cfg->max_pages, cfg->max_streams, cfg->n_kv_heads, ctx->cfg.n_heads))
+    return fail(ctx, CFDETR_ESHAPE, why);
+  Carver cv;
+  const uint64_t o_arrived = cv.take(sizeof(int32_t));
+  hipError_t e = hipMalloc(&ctx->mem_arena, cv.off);
+  if (e != hipSuccess) {
+    ctx->mem_arena = nullptr;
+    return fail(ctx, CFDETR_ENOMEM, "hipMalloc of the memory operators' work space");
+  }
+  char* base = static_cast<char*>(ctx->mem_arena);
+  e = hipMemset(base + o_arrived, 0, sizeof(int32_t));
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) {
+    hipFree(ctx->mem_arena);
+    ctx->mem_arena = nullptr;
+    return fail_hip(ctx, "memory's set-up", e);
+  }
+  ctx->mem_arrived = reinterpret_cast<int32_t*>(base + o_arrived);
+  ctx->mem = *cfg;
+  ctx->mem_page_bits = 0;
+  while ((1 << ctx->mem_page_bits) < cfg->page_size) ++ctx->mem_page_bits;
+  ctx->has_mem = true;
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_memory_advance(cfdetr_ctx* ctx, int32_t B, const int32_t* drop, const int32_t* cu_new,
+                                    int32_t n_new, const int32_t* span, int32_t* span_out,
+                                    const int32_t* table, int32_t* table_out, const int32_t* pool,
+                                    int32_t* pool_out, int32_t* free_pages, int32_t* slots,
+                                    void* hip_stream) {
+  cfdetr_status st = check_memory_call(ctx, B);
+  if (st != CFDETR_OK) return st;
+  if (n_new < 0 || n_new > 1 << 30) return fail(ctx, CFDETR_EINVAL, "n_new must be 0..2^30");
+  if (!cu_new || !span || !span_out || !table || !table_out || !pool || !pool_out || !free_pages || (n_new && !slots))
+    return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if (!aligned4({drop, cu_new, table, table_out, pool, pool_out, free_pages, slots}) || reinterpret_cast<uintptr_t>(span) % 8 ||
+      reinterpret_cast<uintptr_t>(span_out) % 8)
+    return fail(ctx, CFDETR_EINVAL, "a pointer is not aligned");
+  MemoryAdvanceArgs a{};
+  a.drop = drop;
+  a.cu = cu_new;
+  a.B = B;
+  a.n_new = n_new;
+  a.page_bits = ctx->mem_page_bits;
+  a.cols = ctx->mem.max_pages;
+  a.n_pages = ctx->mem.n_pages;
+  a.span = reinterpret_cast<const int2*>(span);
+  a.span_out = reinterpret_cast<int2*>(span_out);
+  a.table = table;
+  a.table_out = table_out;
+  a.pool = pool;
+  a.pool_out = pool_out;
+  a.free = free_pages;
+  a.slots = slots;
+  a.err_flag = ctx->err_flag;
+  a.arrived = ctx->mem_arrived;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_PLAN, launch_memory_advance(a, ctx->cus, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_rotary_axes_table(const cfdetr_rotary_axes_params* params, double* freq, uint8_t* axis) {
+  if (!params || !freq || !axis) return fail_create(CFDETR_EINVAL, "null pointer");
+  if (const char* why = check_rotary_axes(*params, 64, true)) return fail_create(CFDETR_EINVAL, why);
+  rotary_axes_table(*params, freq, axis);
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_rotary_axes(cfdetr_ctx* ctx, const cfdetr_rotary_axes_params* params, const double* freq,
+                                 const uint8_t* axis, const float* pos, int32_t M, const void* q,
+                                 int32_t q_ld, void* q_out, int32_t q_out_ld, float q_scale,
+                                 const void* k, int32_t k_ld, void* k_out, int32_t k_out_ld,
+                                 int32_t k_heads, void* hip_stream) {
+  cfdetr_status st = check_device(ctx);
+  if (st != CFDETR_OK) return st;
+  if (!params) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  const int dh = ctx->cfg.d_model / ctx->cfg.n_heads;
+  if (const char* why = check_rotary_axes(*params, dh, false)) return fail(ctx, CFDETR_EINVAL, why);
+  if (M < 0) return fail(ctx, CFDETR_EINVAL, "M must be >= 0");
+  if (!std::isfinite(q_scale)) return fail(ctx, CFDETR_EINVAL, "q_scale is not a finite number");
+  if (!k != !k_out) return fail(ctx, CFDETR_EINVAL, "k and k_out go together");
+  if (k && (k_heads < 1 || k_heads > ctx->cfg.n_heads)) return fail(ctx, CFDETR_EINVAL, "k_heads must be 1..n_heads");
+  if (M == 0) return CFDETR_OK;
+  if (const char* why = check_axes_pointers(freq, axis, pos)) return fail(ctx, CFDETR_EINVAL, why);
+  const struct { const void* p; int ld, columns; } rows[] = {{q, q_ld, ctx->cfg.d_model}, {q_out, q_out_ld, ctx->cfg.d_model},
+                                                             {k, k_ld, k_heads * dh}, {k_out, k_out_ld, k_heads * dh}};
+  for (int i = 0; i < (k ? 4 : 2); ++i)
+    if (const char* why = check_rows(ctx, rows[i].p, rows[i].ld, rows[i].columns)) return fail(ctx, CFDETR_EINVAL, why);
+  if ((q == q_out && q_ld != q_out_ld) || (k && k == k_out && k_ld != k_out_ld))
+    return fail(ctx, CFDETR_EINVAL, "rows rotated in place keep their distance");
+  TurnRowsArgs a{};
+  a.first = {q, q_out, q_ld, q_out_ld, ctx->cfg.n_heads};
+  if (k) a.second = {k, k_out, k_ld, k_out_ld, k_heads};
+  a.pos = pos;
+  a.freq = freq;
+  a.axis = axis;
+  a.M = M;
+  a.d_head = dh;
+  a.rot_dim = params->rot_dim;
+  a.n_axes = params->n_axes;
+  a.interleaved = params->interleaved != 0;
+  a.scale = q_scale;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_QKV, launch_turn_rows(a, ctx->bf16, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_memory_append(cfdetr_ctx* ctx, const cfdetr_rotary_axes_params* params, const double* freq,
+                                   const uint8_t* axis, const float* pos, int32_t M, const void* k,
+                                   int32_t k_ld, const void* v, int32_t v_ld, const int32_t* slots,
+                                   void* k_cache, int32_t k_cache_ld, void* v_cache,
+                                   int32_t v_cache_ld, void* hip_stream) {
+  cfdetr_status st = check_memory_call(ctx, 1);
+  if (st != CFDETR_OK) return st;
+  const int dh = ctx->cfg.d_model / ctx->cfg.n_heads, columns = ctx->mem.n_kv_heads * dh;
+  if (params)
+    if (const char* why = check_rotary_axes(*params, dh, false)) return fail(ctx, CFDETR_EINVAL, why);
+  if (M < 0) return fail(ctx, CFDETR_EINVAL, "M must be >= 0");
+  if (M == 0) return CFDETR_OK;
+  if (params)
+    if (const char* why = check_axes_pointers(freq, axis, pos)) return fail(ctx, CFDETR_EINVAL, why);
+  if (!slots) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if (!aligned4({slots})) return fail(ctx, CFDETR_EINVAL, "a pointer is not aligned");
+  const struct { const void* p; int ld; } rows[] = {{k, k_ld}, {v, v_ld}, {k_cache, k_cache_ld}, {v_cache, v_cache_ld}};
+  for (const auto& r : rows)
+    if (const char* why = check_rows(ctx, r.p, r.ld, columns)) return fail(ctx, CFDETR_EINVAL, why);
+  TurnRowsArgs a{};
+  a.first = {k, k_cache, k_ld, k_cache_ld, ctx->mem.n_kv_heads};
+  a.second = {v, v_cache, v_ld, v_cache_ld, ctx->mem.n_kv_heads};
+  a.slots = slots;
+  a.n_slots = ctx->mem.n_pages * ctx->mem.page_size;
+  a.err_flag = ctx->err_flag;
+  a.M = M;
+  a.d_head = dh;
+  if (params) {
+    a.pos = pos;
+    a.freq = freq;
+    a.axis = axis;
+    a.rot_dim = params->rot_dim;
+    a.n_axes = params->n_axes;
+    a.interleaved = params->interleaved != 0;
+  }
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_GATHER, launch_turn_rows(a, ctx->bf16, s));
+  return CFDETR_OK;
+}
+
+CFDETR_API cfdetr_status cfdetr_memory_attention(cfdetr_ctx* ctx, const void* q, int32_t q_ld, int32_t B, const void* k_cache,
+                                      int32_t k_cache_ld, const void* v_cache, int32_t v_cache_ld,
+                                      const int32_t* span, const int32_t* table,
+                                      const uint8_t* key_mask, float softmax_scale, void* out,
+                                      int32_t out_ld, void* hip_stream) {
+  cfdetr_status st = check_memory_call(ctx, B);
+  if (st != CFDETR_OK) return st;
+  if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale))
+    return fail(ctx, CFDETR_EINVAL, "softmax_scale must be a number, at least 0");
+  if (!span || !table) return fail(ctx, CFDETR_EINVAL, "null pointer");
+  if (!aligned4({table}) || reinterpret_cast<uintptr_t>(span) % 8) return fail(ctx, CFDETR_EINVAL, "a pointer is not aligned");
+  const int d = ctx->cfg.d_model, dh = d / ctx->cfg.n_heads, columns = ctx->mem.n_kv_heads * dh;
+  const struct { const void* p; int ld, columns; } rows[] = {{q, q_ld, d}, {out, out_ld, d}, {k_cache, k_cache_ld, columns}, {v_cache, v_cache_ld, columns}};
+  for (const auto& r : rows)
+    if (const char* why = check_rows(ctx, r.p, r.ld, r.columns)) return fail(ctx, CFDETR_EINVAL, why);
+  if (q == out && q_ld != out_ld) return fail(ctx, CFDETR_EINVAL, "rows written in place keep their distance");
+  MemoryAttentionArgs a{};
+  a.q = q;
+  a.k = k_cache;
+  a.v = v_cache;
+  a.out = out;
+  a.q_ld = q_ld;
+  a.k_ld = k_cache_ld;
+  a.v_ld = v_cache_ld;
+  a.out_ld = out_ld;
+  a.B = B;
+  a.heads = ctx->cfg.n_heads;
+  a.kv_heads = ctx->mem.n_kv_heads;
+  a.page_bits = ctx->mem_page_bits;
+  a.cols = ctx->mem.max_pages;
+  a.n_pages = ctx->mem.n_pages;
+  a.span = reinterpret_cast<const int2*>(span);
+  a.table = table;
+  a.mask = key_mask;
+  a.scale2 = softmax_scale > 0.f ? softmax_scale * 1.44269504088896340736f : 1.0f;
+  a.err_flag = ctx->err_flag;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  CF_LAUNCH(CFDETR_K_ATTN, launch_memory_attention(a, dh, ctx->bf16, s));
   return CFDETR_OK;
 }
 

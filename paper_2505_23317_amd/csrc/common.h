@@ -98,6 +98,20 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Sum of v over this lane and those before it: inside the vector unit, within rows of 16, then row 0 into 1 and 2 into 3,
+// then 1 into 2 and 3.
+__device__ __forceinline__ int sum_upto(int v) {
+  auto from = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+  const auto all = std::integral_constant<int, 0xF>{};
+  v += from(std::integral_constant<int, 0x111>{}, all);   // row_shr:1, 2, 4, 8
+  v += from(std::integral_constant<int, 0x112>{}, all);
+  v += from(std::integral_constant<int, 0x114>{}, all);
+  v += from(std::integral_constant<int, 0x118>{}, all);
+  v += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
+  v += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
+  return v;
+}
+
 // LayerNorm of a row that a wavefront holds in quads of columns (quad lane + 64 j in v[j],
 // zeros beyond `quads`): mean first, then the variance of the centred values.  Fused
 // multiply-adds are written out, so that every kernel that does this gets the same bits.

@@ -32,19 +32,6 @@ __device__ __forceinline__ Frames frames_of(const int32_t* __restrict__ cu_q, co
   f.bad = __any(bad || (l == 0 && (f.q[0] != 0 || f.k[0] != 0)));
   return f;
 }
-// Sum of v over this lane and those before it: inside the vector unit, within rows of 16, then row 0 into 1 and 2 into 3,
-// then 1 into 2 and 3.
-__device__ __forceinline__ int sum_upto(int v) {
-  auto from = [&](auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
-  const auto all = std::integral_constant<int, 0xF>{};
-  v += from(std::integral_constant<int, 0x111>{}, all);   // row_shr:1, 2, 4, 8
-  v += from(std::integral_constant<int, 0x112>{}, all);
-  v += from(std::integral_constant<int, 0x114>{}, all);
-  v += from(std::integral_constant<int, 0x118>{}, all);
-  v += from(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
-  v += from(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
-  return v;
-}
 // The frame that piece `id` belongs to, where a frame has pieces[0 or 1] of them (lane's two frames, `upto` their sum_upto); `id`
 // becomes the piece's number within it.  -1: there are fewer.
 __device__ __forceinline__ int frame_of_piece(const int (&pieces)[2], int upto, int& id) {

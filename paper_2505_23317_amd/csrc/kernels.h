@@ -492,4 +492,58 @@ struct NormResidualArgs {
 };
 hipError_t launch_norm_residual(const NormResidualArgs& a, bool block_is_bf16, bool normed_is_bf16, int m_capacity, hipStream_t s);
 
+// ---- paged stream memory (memory_advance.hip, memory_rows.hip, memory_attention.hip; stream_memory.h) --------
+// span [B] = (first, held), table [B, cols], pool = (head, number of free pages), free [n_pages] a ring; cu [B + 1], drop [B] or
+// null, slots [n_new] out.  The outputs may be the inputs.  A step that cannot be made sets *err_flag and leaves the state as
+// it was.  arrived: a counter that is 0 between calls.
+struct MemoryAdvanceArgs {
+  const int32_t *drop, *cu;
+  int B, n_new, page_bits, cols, n_pages;
+  const int2* span;
+  int2* span_out;
+  const int32_t* table;
+  int32_t* table_out;
+  const int32_t* pool;
+  int32_t* pool_out;
+  int32_t *free, *slots, *err_flag, *arrived;
+};
+hipError_t launch_memory_advance(const MemoryAdvanceArgs& a, int cus, hipStream_t s);
+
+// Rows of two parts, `heads` heads of d_head each.  Without slots both are turned (the first also scaled) and written
+// row by row, an output may be its input; with slots the first is turned, the second copied, and both go to row slots[m] of the
+// outputs (none where that is negative; n_slots or more sets *err_flag too).  pos [M, n_axes], freq and axis [rot_dim / 2].
+struct TurnRowsPart {
+  const void* in;
+  void* out;
+  int in_ld, out_ld, heads;
+};
+struct TurnRowsArgs {
+  TurnRowsPart first, second;
+  const float* pos;
+  const double* freq;
+  const uint8_t* axis;
+  const int32_t* slots;
+  int32_t* err_flag;
+  int M, n_slots, d_head, rot_dim, n_axes;
+  bool interleaved;
+  float scale;
+};
+hipError_t launch_turn_rows(const TurnRowsArgs& a, bool use_bf16, hipStream_t s);
+
+// One query row of every stream, `heads` heads of d_head, over the tokens that the stream holds: kv_heads key heads, each read by
+// heads / kv_heads query heads; keys and values [n_pages * page, ld] by slot, mask [n_pages * page] or null.  A span that no step
+// leaves sets *err_flag and nothing is written; a page number that is none sets it too and is not read.
+struct MemoryAttentionArgs {
+  const void *q, *k, *v;
+  void* out;
+  int q_ld, k_ld, v_ld, out_ld;
+  int B, heads, kv_heads, page_bits, cols, n_pages;
+  const int2* span;
+  const int32_t* table;
+  const uint8_t* mask;
+  float scale2;   // of the logits, in base 2
+  int32_t* err_flag;
+};
+hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
+
 }  // namespace cfdetr
