@@ -685,9 +685,9 @@ CFDETR_API cfdetr_status cfdetr_memory_append(cfdetr_ctx* ctx, const cfdetr_rota
  * Attention of one new token of every stream over all that the stream holds (its own key and value among it, once they are appended):
  * with G = n_heads / n_kv_heads, head h of out is softmax(softmax_scale q_h k_g^T) v_g over the held tokens, g = h / G.
  *   q       [B, ld] act: n_heads heads
- *   span, table  as a step leaves them.  A span that no step leaves makes the call write nothing; a page number outside 0 .. n_pages - 1
+ *   span, table  as a step leaves them.  A span that no step leaves, or 2^35 tokens and more in all, makes the call write nothing; a page number outside 0 .. n_pages - 1
  *           is not read (its tokens count as masked).  Both are reported by cfdetr_sync_status as CFDETR_ECAPACITY.
- *   key_mask  [n_pages * page_size] uint8 device, by slot, 0: the token is not read, whatever it holds; NULL: all are read
+ *   key_mask  [n_pages * page_size] uint8 device (8-byte aligned), by slot, 0: the token is not read, whatever it holds; NULL: all are read
  *   softmax_scale  > 0; or 0: the queries have been multiplied by log2(e) / sqrt(d_head) already
  *   out     [B, ld] act; may be q (with the same ld).  The row of a stream that holds no token that may be read is 0.
  * Sums are 32-bit, of weights of up to 2^16 (the elements of v are taken to be below 2^110 / n in size for n tokens).  A v that

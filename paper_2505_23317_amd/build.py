@@ -22,7 +22,8 @@ FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-fvisibility=hi
 # GEMMs only read theirs in the epilogue and are faster with AGPR accumulators.
 EXTRA_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "diff_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "diff_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "diff_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "memory_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:

@@ -120,6 +120,10 @@ struct cfdetr_ctx {
   int mem_page_bits = 0;
   void* mem_arena = nullptr;
   int32_t* mem_arrived = nullptr;   // counter of workgroups, 0 between calls
+  int32_t* mem_tickets = nullptr;   // counters of the attention's pieces, 0 between calls
+  void* mem_zeros = nullptr;        // 16 bytes of 0
+  float2* mem_ml = nullptr;         // the pieces' maxima and sums, and their rows
+  float* mem_rows = nullptr;
 
   std::string err;
 
@@ -2022,14 +2026,16 @@ CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memo
   if (const char* why = check_memory_sizes(cfg->page_size, cfg->n_pages, cfg->max_pages, cfg->max_streams, cfg->n_kv_heads, ctx->cfg.n_heads))
     return fail(ctx, CFDETR_ESHAPE, why);
   Carver cv;
-  const uint64_t o_arrived = cv.take(sizeof(int32_t));
+  const MemoryAttentionSpace space = memory_attention_space(cfg->max_streams, ctx->cfg.n_heads, ctx->cfg.d_model / ctx->cfg.n_heads, ctx->cus);
+  const uint64_t o_arrived = cv.take(sizeof(int32_t)), o_zeros = cv.take(16), o_tickets = cv.take(space.tickets), cleared = cv.off;
+  const uint64_t o_ml = cv.take(space.ml), o_rows = cv.take(space.rows);
   hipError_t e = hipMalloc(&ctx->mem_arena, cv.off);
   if (e != hipSuccess) {
     ctx->mem_arena = nullptr;
     return fail(ctx, CFDETR_ENOMEM, "hipMalloc of the memory operators' work space");
   }
   char* base = static_cast<char*>(ctx->mem_arena);
-  e = hipMemset(base + o_arrived, 0, sizeof(int32_t));
+  e = hipMemset(base, 0, cleared);
   if (e == hipSuccess) e = hipDeviceSynchronize();
   if (e != hipSuccess) {
     hipFree(ctx->mem_arena);
@@ -2037,6 +2043,10 @@ CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memo
     return fail_hip(ctx, "memory's set-up", e);
   }
   ctx->mem_arrived = reinterpret_cast<int32_t*>(base + o_arrived);
+  ctx->mem_tickets = reinterpret_cast<int32_t*>(base + o_tickets);
+  ctx->mem_zeros = base + o_zeros;
+  ctx->mem_ml = reinterpret_cast<float2*>(base + o_ml);
+  ctx->mem_rows = reinterpret_cast<float*>(base + o_rows);
   ctx->mem = *cfg;
   ctx->mem_page_bits = 0;
   while ((1 << ctx->mem_page_bits) < cfg->page_size) ++ctx->mem_page_bits;
@@ -2176,7 +2186,7 @@ CFDETR_API cfdetr_status cfdetr_memory_attention(cfdetr_ctx* ctx, const void* q,
   if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale))
     return fail(ctx, CFDETR_EINVAL, "softmax_scale must be a number, at least 0");
   if (!span || !table) return fail(ctx, CFDETR_EINVAL, "null pointer");
-  if (!aligned4({table}) || reinterpret_cast<uintptr_t>(span) % 8) return fail(ctx, CFDETR_EINVAL, "a pointer is not aligned");
+  if (!aligned4({table}) || reinterpret_cast<uintptr_t>(span) % 8 || reinterpret_cast<uintptr_t>(key_mask) % 8) return fail(ctx, CFDETR_EINVAL, "a pointer is not aligned");
   const int d = ctx->cfg.d_model, dh = d / ctx->cfg.n_heads, columns = ctx->mem.n_kv_heads * dh;
   const struct { const void* p; int ld, columns; } rows[] = {{q, q_ld, d}, {out, out_ld, d}, {k_cache, k_cache_ld, columns}, {v_cache, v_cache_ld, columns}};
   for (const auto& r : rows)
@@ -2202,8 +2212,12 @@ CFDETR_API cfdetr_status cfdetr_memory_attention(cfdetr_ctx* ctx, const void* q,
   a.mask = key_mask;
   a.scale2 = softmax_scale > 0.f ? softmax_scale * 1.44269504088896340736f : 1.0f;
   a.err_flag = ctx->err_flag;
+  a.partial_ml = ctx->mem_ml;
+  a.partial = ctx->mem_rows;
+  a.tickets = ctx->mem_tickets;
+  a.zeros = ctx->mem_zeros;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  CF_LAUNCH(CFDETR_K_ATTN, launch_memory_attention(a, dh, ctx->bf16, s));
+  CF_LAUNCH(CFDETR_K_ATTN, launch_memory_attention(a, dh, ctx->bf16, ctx->cus, s));
   return CFDETR_OK;
 }
 

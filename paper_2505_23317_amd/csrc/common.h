@@ -112,6 +112,15 @@ __device__ __forceinline__ int sum_upto(int v) {
   return v;
 }
 
+// One 16-byte piece per lane from global memory straight into LDS (1 KB a wavefront at lds_addr, in lane order).  The
+// compiler does not count these loads: whoever reads them waits with vmcnt first.
+__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(sbase) : "memory");
+}
+__device__ __forceinline__ void dma16(const void* from, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(from) : "memory");
+}
+
 // LayerNorm of a row that a wavefront holds in quads of columns (quad lane + 64 j in v[j],
 // zeros beyond `quads`): mean first, then the variance of the centred values.  Fused
 // multiply-adds are written out, so that every kernel that does this gets the same bits.

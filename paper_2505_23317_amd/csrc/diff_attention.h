@@ -255,14 +255,6 @@ __device__ __forceinline__ void unit_rows(const unsigned char* sV, const f32x16 
   }
 }
 
-// One 16-byte piece per lane from global memory straight into LDS (1 KB a wavefront at lds_addr, in lane order).  The
-// compiler does not count these loads: whoever reads them waits with vmcnt first.
-__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(voff), "s"(sbase) : "memory");
-}
-__device__ __forceinline__ void dma16(const void* from, uint32_t lds_addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(from) : "memory");
-}
 // Which chunk of 16 bytes lies at place `c` of an LDS row of keys, and of values (both orders are their own inverse).
 template <typename T, int ROWB>
 __device__ __forceinline__ int key_piece(int row, int c) { return key_chunk<T, ROWB>(row, c); }

@@ -543,7 +543,17 @@ struct MemoryAttentionArgs {
   const uint8_t* mask;
   float scale2;   // of the logits, in base 2
   int32_t* err_flag;
+  // work space (memory_attention_space); tickets are 0 between calls, zeros are 16 bytes of 0
+  float2* partial_ml;
+  float* partial;
+  int32_t* tickets;
+  const void* zeros;
+  int ranges, wave_slabs;   // the launcher's
 };
-hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s);
+struct MemoryAttentionSpace {
+  uint64_t ml, rows, tickets;   // bytes
+};
+MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus);
+hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, int cus, hipStream_t s);
 
 }  // namespace cfdetr

@@ -3,6 +3,15 @@
 //
 // One pass over keys and values, with a running maximum and sum.  Every key and value is read once for the G query
 // heads that share it: 2 G operations a byte in bf16, so memory bounds it.
+//
+// The tokens of all streams are one row of units of 32 positions, cut into ranges of one length, a workgroup each (lengths are
+// known on the device only, so every workgroup adds the streams' units up for itself).  A range may end inside a stream and
+// hold several: every piece of a stream gives a row under its own maximum; a stream that lies in one range is
+// finished there, the pieces of the others go to memory and the workgroup that ends last adds them up in order.
+// Units lie on multiples of 32 positions and pages hold 8 or more, so eight consecutive tokens of a unit are in one page.
+#include <algorithm>
+#include <type_traits>
+
 #include "kernels.h"
 #include "stream_memory.h"
 
@@ -10,163 +19,570 @@ namespace cfdetr {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kUnit = 32;             // tokens
+constexpr int kMostUnits = 1 << 30;   // of all streams
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// 16 bytes of a row as numbers, and their products with a query's.
-template <typename T>
-struct Piece;
-template <>
-struct Piece<bf16_t> {
-  static constexpr int kN = 8;
-  static __device__ __forceinline__ void get(const uint4& v, float (&x)[kN]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Tiles' page numbers and open tokens, those of up to 64 of a wavefront's tiles at a time: lane l has tile l's.
+struct Tiles {
+  int id[4];       // page of tokens 8 j .. 8 j + 7
+  uint32_t open;   // bit t: token t is read
+};
+__device__ __forceinline__ Tiles tiles_of(const MemoryAttentionArgs& a, const int32_t* table, int first, int end, int p0, bool any) {
+  Tiles t{};
+  if (!any) return t;
+  const int lo = max(first - p0, 0), hi = min(end - p0, kUnit);
+  t.open = (0xFFFFFFFFu >> (kUnit - hi)) & (0xFFFFFFFFu << lo);
+  bool wrong = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  for (int j = 0; j < 4; ++j) {
+    if ((t.open >> (8 * j) & 0xFF) == 0) continue;
+    t.id[j] = table[ring_column((p0 + 8 * j) >> a.page_bits, a.cols)];
+  }
+  uint2 bytes[4] = {};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if ((unsigned)t.id[j] >= (unsigned)a.n_pages) {
+      wrong = true;
+      t.id[j] = 0;
+      t.open &= ~(0xFFu << (8 * j));
+    }
+    if (a.mask) bytes[j] = *reinterpret_cast<const uint2*>(a.mask + ((size_t)t.id[j] << a.page_bits) + ((p0 + 8 * j) & ((1 << a.page_bits) - 1)));
+  }
+  if (a.mask) {
+    uint32_t read = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (bytes[j].x >> (8 * i) & 0xFF) read |= 1u << (8 * j + i);
+        if (bytes[j].y >> (8 * i) & 0xFF) read |= 1u << (8 * j + 4 + i);
+      }
+    t.open &= read;
+  }
+  if (wrong) *a.err_flag = 1;
+  return t;
+}
+
+// Maximum and sum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
+template <typename F>
+__device__ __forceinline__ float across_quarters(float v, F f) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  u32x2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
+// The reference of the weights follows the largest logit only once that is kSlack ahead (in base 2): rows under the reference are
+// multiplied less often.  A weight is 2^kSlack at most; the header promises sums for values below 2^110 / n.
+constexpr float kSlack = 16.f;
+
+// What a wavefront leaves of its tiles: for row i of its kRows (query heads) a maximum, a sum and a row under that maximum.
+template <int ROWS, int DH>
+struct Rows {
+  float m[ROWS], l[ROWS];
+  float o[ROWS][DH];
+};
+
+// bf16.  A wavefront has 128 bytes of every key and value row, a slab: NH key heads, and up to 16 query heads of each.
+// Logits are products of 16 tokens x 32 features x 16 query heads, S^T = K Q^T, which leave lane l query head l mod 16 and tokens
+// 4 (l / 16) + r of either half of the tile; these are at once the operand of O^T = V^T P^T if the products' index runs over
+// the tokens in that order, so weights never leave their lane.  With one query head of 16 the products are 15 parts zeros and still cost a
+// fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own; keys of the next tile are asked
+// for when the logits are taken, values when the row is: no barrier in the loop.
+template <int DH>
+struct Core16 {
+  typedef bf16_t T;
+  static constexpr int kSlabHeads = 64 / DH, kGroup = 16, kRows = kSlabHeads * kGroup;
+  static constexpr int kBytes = 2 * kUnit * 128;   // LDS: keys, values
+  typedef Rows<kRows, DH> Result;
+  static_assert(sizeof(Result) <= kBytes, "in place of keys and values");
+
+  static __device__ __forceinline__ void run(const MemoryAttentionArgs& a, unsigned char* lds, int b, int slab, int group, int unit, int step,
+                                             int units, int first, int end) {
+    constexpr int NH = kSlabHeads, KS = DH / 32, NB = DH / 16;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    const int G = a.heads / a.kv_heads;
+    const int32_t* const table = a.table + (size_t)b * a.cols;
+    // the queries' operand: query head l16 of either key head
+    uint4 qf[NH][KS];
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const int kh = slab * NH + h, head = group * kGroup + l16;
+      const bool mine = kh < a.kv_heads && head < G;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        qf[h][s] = make_uint4(0, 0, 0, 0);
+        if (mine) qf[h][s] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)b * a.q_ld + (kh * G + head) * DH + 32 * s + 8 * g);
+      }
+    }
+    f32x4 acc[NH][NB];
+    float m_run[NH], l_run[NH];
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      m_run[h] = -INFINITY;
+      l_run[h] = 0.f;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[h][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // Loads: lane l has place l mod 8 of token 8 j + l / 8.  A row's pieces of 16 bytes lie in LDS so that what is read together
+    // lies in different banks: key piece c of token t at place c ^ (t / 2 mod 8), values in pairs of pieces, pair c at c ^ (t / 2 mod 4).
+    const bool half = (slab + 1) * NH > a.kv_heads;   // (the slab's second key head is none: its first again)
+    const int kc = (lane & 7) ^ g, vc = ((((lane & 7) >> 1) ^ g) << 1) | (lane & 1);
+    const uint32_t k_step = (uint32_t)a.k_ld * 2, v_step = (uint32_t)a.v_ld * 2;
+    const uint32_t k_lane = (uint32_t)(lane >> 3) * k_step + slab * 128, v_lane = (uint32_t)(lane >> 3) * v_step + slab * 128;
+    const uint32_t k_even = k_lane + (half ? kc & 3 : kc) * 16, k_odd = k_lane + (half ? kc & 3 : kc ^ 4) * 16;
+    const uint32_t v_off = v_lane + (half ? vc & 3 : vc) * 16;
+    unsigned char* const sK = lds;
+    unsigned char* const sV = lds + kUnit * 128;
+    const uint32_t ldsK = (uint32_t)(uintptr_t)sK, ldsV = ldsK + kUnit * 128;
+    const int p_first = first & ~(kUnit - 1), page_mask = (1 << a.page_bits) - 1;
+
+#pragma nounroll
+    for (; unit < units; unit += 64 * step) {
+      const int count = min(64, (units - unit + step - 1) / step);
+      const int p_lane = p_first + (unit + lane * step) * kUnit;
+      Tiles t = tiles_of(a, table, first, end, p_lane, lane < count);
+      // (ordinary loads are waited for here: the compiler does not count those into LDS, and would wait for all of them below)
+      asm volatile("" : "+v"(t.id[0]), "+v"(t.id[1]), "+v"(t.id[2]), "+v"(t.id[3]), "+v"(t.open));
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[h][s].x), "+v"(qf[h][s].y), "+v"(qf[h][s].z), "+v"(qf[h][s].w));
+
+      auto load = [&](const void* base, uint32_t row, uint32_t even, uint32_t odd, int i, uint32_t to) {
+        const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
+        const int p0 = p_first + (unit + i * step) * kUnit;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int id = __builtin_amdgcn_readlane(t.id[j], i);
+          const size_t slot = ((size_t)id << a.page_bits) + ((p0 + 8 * j) & page_mask);
+          const char* const from = static_cast<const char*>(base) + slot * row;
+          const uint32_t off = j & 1 ? odd : even;
+          if (open == 0xFFFFFFFFu) {
+            dma16(from, off, to + j * 1024);
+          } else {
+            // tokens that are not read: zeros, from the one place that all such lanes share
+            const bool read = open >> (8 * j + (lane >> 3)) & 1;
+            dma16(read ? from + off : static_cast<const char*>(a.zeros), to + j * 1024);
+          }
+        }
+      };
+      load(a.k, k_step, k_even, k_odd, 0, ldsK);
+      load(a.v, v_step, v_off, v_off, 0, ldsV);
+#pragma nounroll
+      for (int i = 0; i < count; ++i) {
+        const bool more = i + 1 < count;
+        asm volatile("s_waitcnt vmcnt(4)" : : : "memory");   // the keys; their values need not be there yet
+        f32x4 s[NH][2];
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int half16 = 0; half16 < 2; ++half16) {
+            const int row = 16 * half16 + l16;
+            s[h][half16] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+              const int piece = (h * KS + c) * 4 + g;
+              const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sK + row * 128 + (piece ^ ((row >> 1) & 7)) * 16);
+              s[h][half16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, *reinterpret_cast<const bf16x8*>(&qf[h][c]), s[h][half16], 0, 0, 0);
+            }
+          }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        if (more) load(a.k, k_step, k_even, k_odd, i + 1, ldsK);
+        const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
+        bf16x8 w[NH];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+          if (open != 0xFFFFFFFFu) {
+            const uint32_t mine = open >> (4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              if (!(mine >> r & 1)) s[h][0][r] = -INFINITY;
+              if (!(mine >> (16 + r) & 1)) s[h][1][r] = -INFINITY;
+            }
+          }
+          float top = s[h][0][0];
+#pragma unroll
+          for (int r = 1; r < 8; ++r) top = fmaxf(top, s[h][r >> 2][r & 3]);
+          top = across_quarters(top, [](float x, float y) { return fmaxf(x, y); }) * a.scale2;
+          const bool follow = top > m_run[h] + kSlack;
+          if (__any(follow)) {
+            const float alpha = follow ? __builtin_amdgcn_exp2f(m_run[h] - top) : 1.0f;
+            if (follow) m_run[h] = top;
+            l_run[h] *= alpha;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[h][n] *= alpha;
+          }
+          const float ref = m_run[h] == -INFINITY ? 0.f : m_run[h];   // (no token may be open so far)
+          float p[8], sum = 0.f;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            p[r] = __builtin_amdgcn_exp2f(fmaf(s[h][r >> 2][r & 3], a.scale2, -ref));
+            sum += p[r];
+          }
+          l_run[h] += sum;
+          // a rounding of the weights: half a step of 2^-8 each, the sum takes them as they were
+          const uint4 packed = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+          w[h] = *reinterpret_cast<const bf16x8*>(&packed);
+        }
+        if (more) asm volatile("s_waitcnt vmcnt(4)" : : : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        typedef __attribute__((ext_vector_type(4))) short s16x4;
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+            // the transposing read gives a lane four tokens of its column, 16 lanes naming the pieces of four tokens by 16 columns
+            union {
+              s16x4 part[2];
+              bf16x8 whole;
+            } v;
+#pragma unroll
+            for (int half16 = 0; half16 < 2; ++half16) {
+              const int row = 16 * half16 + 4 * g + (l16 >> 2);
+              v.part[half16] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (lds4)(sV + row * 128 + ((h * NB + n) ^ ((row >> 1) & 3)) * 32 + (lane & 3) * 8));
+            }
+            acc[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.whole, w[h], acc[h][n], 0, 0, 0);
+          }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        if (more) load(a.v, v_step, v_off, v_off, i + 1, ldsV);
+      }
+    }
+    // (the LDS of keys and values is free: every read has been waited for)
+    Result* const to = reinterpret_cast<Result*>(lds);
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const float l = across_quarters(l_run[h], [](float x, float y) { return x + y; });
+      const int row = h * kGroup + l16;
+      if (group * kGroup + l16 >= G) continue;
+      if (g == 0) {
+        to->m[row] = m_run[h];
+        to->l[row] = l;
+      }
+#pragma unroll
+      for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(&to->o[row][16 * n + 4 * g]) = acc[h][n];
     }
   }
-  static __device__ __forceinline__ uint4 put(const float (&x)[kN]) {
-    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-  }
 };
-template <>
-struct Piece<float> {
-  static constexpr int kN = 4;
-  static __device__ __forceinline__ void get(const uint4& v, float (&x)[kN]) {
-    x[0] = __uint_as_float(v.x);
-    x[1] = __uint_as_float(v.y);
-    x[2] = __uint_as_float(v.z);
-    x[3] = __uint_as_float(v.w);
-  }
-  static __device__ __forceinline__ uint4 put(const float (&x)[kN]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+
+// fp32, the check mode: a wavefront has one key head and up to four query heads.  LPR lanes hold a row's pieces of 16 bytes, so
+// a load takes 64 / LPR tokens; each group of lanes has a maximum, sum and row of its own until the end.
+template <int DH>
+struct Core32 {
+  typedef float T;
+  static constexpr int kSlabHeads = 1, kGroup = 4, kRows = kGroup;
+  typedef Rows<kRows, DH> Result;
+  static constexpr int kBytes = (sizeof(Result) + 255) / 256 * 256;
+
+  static __device__ __forceinline__ void run(const MemoryAttentionArgs& a, unsigned char* lds, int b, int slab, int group, int unit, int step,
+                                             int units, int first, int end) {
+    constexpr int LPR = DH / 4, TPL = 64 / LPR, LOADS = kUnit / TPL;
+    const int lane = threadIdx.x & 63, part = lane / LPR, c = lane % LPR;
+    const int G = a.heads / a.kv_heads;
+    const int32_t* const table = a.table + (size_t)b * a.cols;
+    float4 q[kGroup], acc[kGroup];
+    float m[kGroup], l[kGroup];
+#pragma unroll
+    for (int h = 0; h < kGroup; ++h) {
+      const int head = slab * G + min(group * kGroup + h, G - 1);   // (a group's last head again, where there are fewer)
+      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (size_t)b * a.q_ld + head * DH + 4 * c);
+      q[h] = make_float4(v.x * a.scale2, v.y * a.scale2, v.z * a.scale2, v.w * a.scale2);
+      acc[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+      m[h] = -INFINITY;
+      l[h] = 0.f;
+    }
+    const int p_first = first & ~(kUnit - 1), page_mask = (1 << a.page_bits) - 1;
+    for (; unit < units; unit += 64 * step) {
+      const int count = min(64, (units - unit + step - 1) / step);
+      const Tiles t = tiles_of(a, table, first, end, p_first + (unit + lane * step) * kUnit, lane < count);
+      for (int i = 0; i < count; ++i) {
+        const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
+        const int p0 = p_first + (unit + i * step) * kUnit;
+        float4 k[LOADS], v[LOADS];
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const int token = j * TPL + part;
+          const int id = __builtin_amdgcn_readlane(t.id[j * TPL / 8], i);
+          const size_t slot = ((size_t)id << a.page_bits) + ((p0 + token) & page_mask);
+          k[j] = v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (open >> token & 1) {
+            k[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.k) + slot * a.k_ld + slab * DH + 4 * c);
+            v[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.v) + slot * a.v_ld + slab * DH + 4 * c);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < kGroup; ++h) {
+          float s[LOADS], top = m[h];
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) {
+            s[j] = fmaf(q[h].x, k[j].x, fmaf(q[h].y, k[j].y, fmaf(q[h].z, k[j].z, q[h].w * k[j].w)));
+#pragma unroll
+            for (int o = 1; o < LPR; o <<= 1) s[j] += __shfl_xor(s[j], o);
+            if (!(open >> (j * TPL + part) & 1)) s[j] = -INFINITY;
+            top = fmaxf(top, s[j]);
+          }
+          const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(m[h] - ref);
+          m[h] = top;
+          l[h] *= keep;
+          acc[h] = make_float4(acc[h].x * keep, acc[h].y * keep, acc[h].z * keep, acc[h].w * keep);
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) {
+            const float w = __builtin_amdgcn_exp2f(s[j] - ref);
+            l[h] += w;
+            acc[h] = make_float4(fmaf(w, v[j].x, acc[h].x), fmaf(w, v[j].y, acc[h].y), fmaf(w, v[j].z, acc[h].z), fmaf(w, v[j].w, acc[h].w));
+          }
+        }
+      }
+    }
+    Result* const to = reinterpret_cast<Result*>(lds);
+#pragma unroll
+    for (int h = 0; h < kGroup; ++h) {
+      float top = m[h];
+#pragma unroll
+      for (int o = LPR; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      const float f = __builtin_amdgcn_exp2f(m[h] - (top == -INFINITY ? 0.f : top));
+      float sums[5] = {l[h] * f, acc[h].x * f, acc[h].y * f, acc[h].z * f, acc[h].w * f};
+#pragma unroll
+      for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) sums[i] += __shfl_xor(sums[i], o);
+      if (part == 0) {
+        if (c == 0) {
+          to->m[h] = top;
+          to->l[h] = sums[0];
+        }
+        *reinterpret_cast<float4*>(&to->o[h][4 * c]) = make_float4(sums[1], sums[2], sums[3], sums[4]);
+      }
+    }
   }
 };
 
-// A workgroup has a stream, a key head and up to GP of its query heads.  LPH lanes hold a row's 16-byte pieces, so that a
-// wavefront takes 64 / LPH tokens at a time, each group of lanes with a running maximum, sum and row of its own; the groups'
-// results are brought to one maximum and added at the end.
-template <typename T, int DH, int GP>
-__global__ __launch_bounds__(kThreads) void memory_attention_kernel(MemoryAttentionArgs a) {
-  constexpr int N = Piece<T>::kN, LPH = DH / N, TPW = 64 / LPH;
-  __shared__ float s_m[kWaves][TPW][GP], s_l[kWaves][TPW][GP];
-  __shared__ float s_o[kWaves][TPW][GP][DH];
-  __shared__ int s_bad;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b = blockIdx.x, kh = blockIdx.y, G = a.heads / a.kv_heads;
-  if (tid == 0) s_bad = 0;
+template <typename T>
+__device__ __forceinline__ void store4(T* to, float4 x) {
+  if constexpr (std::is_same_v<T, float>) *reinterpret_cast<float4*>(to) = x;
+  else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(x.x, x.y), pack_bf16x2(x.z, x.w));
+}
+
+// Pieces pass between workgroups of any XCD, whose L2s do not see each other's: every one is written past them (stores of device
+// scope, waited for before the workgroup is counted) and read past them.  A release and an acquire around the counter would do the
+// same for all of an L2: one stream of 200,003 tokens, width 768, 116 us so, 267 with them.
+__device__ __forceinline__ void put2(float2* to, float2 v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get2(const float2* from) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+// Four columns of a row under a maximum.
+struct Sum {
+  float m, l;
+  float4 o;
+  __device__ __forceinline__ void add(const Sum& s) {
+    const float top = fmaxf(m, s.m), ref = top == -INFINITY ? 0.f : top;
+    const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(s.m - ref);
+    m = top;
+    l = fmaf(l, f, s.l * g);
+    o = make_float4(fmaf(o.x, f, s.o.x * g), fmaf(o.y, f, s.o.y * g), fmaf(o.z, f, s.o.z * g), fmaf(o.w, f, s.o.w * g));
+  }
+};
+// First query head of a slab: slabs go through the key heads and, where a key head has more query heads than a wavefront takes,
+// through groups of these, so that the query heads of consecutive slabs lie behind each other.
+template <typename Core>
+__device__ __forceinline__ int first_head(int slab, int passes, int G) {
+  return slab / passes * Core::kSlabHeads * G + slab % passes * Core::kGroup;
+}
+
+// LDS of a workgroup in front of the streams' units: the wavefronts', or the sums of a stream's pieces.
+template <typename Core, int NW>
+constexpr int kLds = std::max(NW * Core::kBytes, 64 * NW * (int)sizeof(Sum));
+
+// Workgroup: one of `a.ranges` ranges of units and a.wave_slabs of the slabs; its NW wavefronts have one slab each, and where
+// that leaves some over, every second, third, .. tile of it.
+template <typename Core, int DH, int NW>
+__global__ __launch_bounds__(64 * NW, 4) void memory_attention_kernel(MemoryAttentionArgs a) {
+  typedef typename Core::T T;
+  typedef typename Core::Result Result;
+  constexpr int kThreads = 64 * NW;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  __shared__ int s_wave[2][NW], s_flag;
+  int* const s_units = reinterpret_cast<int*>(smem + kLds<Core, NW>);   // [B + 1] exclusive sums of the streams' units
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = uniform(tid >> 6);
+  const int B = a.B, G = a.heads / a.kv_heads;
+
+  // units of every stream, and their sums
+  if (tid == 0) s_flag = 0;
   __syncthreads();
-  for (int i = tid; i < a.B; i += kThreads) {
-    const int2 span = a.span[i];
-    if (span_is_bad(span.x, span.y, a.page_bits, a.cols)) s_bad = 1;
+  const int per = (B + kThreads - 1) / kThreads, b0 = tid * per, b1 = min(B, b0 + per);
+  int mine = 0;
+  bool bad = false;
+  for (int b = b0; b < b1; ++b) {
+    const int2 span = a.span[b];
+    const bool wrong = span_is_bad(span.x, span.y, a.page_bits, a.cols);
+    s_units[b] = mine;
+    bad |= wrong;
+    if (!wrong && span.y > 0) mine += ((span.x + span.y - 1) / kUnit) - span.x / kUnit + 1;
+  }
+  if (bad) s_flag = 1;
+  // (a thread's units are below 2^28; their thousands tell whether the sum fits 32 bits)
+  const int upto = sum_upto(mine), thousands = sum_upto((mine + 1023) / 1024);
+  if (lane == 63) {
+    s_wave[0][wave] = upto;
+    s_wave[1][wave] = thousands;
   }
   __syncthreads();
-  if (s_bad) {
-    if (tid == 0) *a.err_flag = 1;
+  int base = upto - mine, total = 0, all_thousands = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    if (w < wave) base += s_wave[0][w];
+    total += s_wave[0][w];
+    all_thousands += s_wave[1][w];
+  }
+  total = uniform(total);
+  if (s_flag || all_thousands > kMostUnits / 1024) {
+    if (blockIdx.x == 0 && tid == 0) *a.err_flag = 1;
     return;
   }
-  const int first = a.span[b].x, held = a.span[b].y;
-  const int group = lane / LPH, c = lane % LPH;
-  float q[GP][N], acc[GP][N], m[GP], l[GP];
-  int head[GP];
-#pragma unroll
-  for (int g = 0; g < GP; ++g) {
-    head[g] = kh * G + min((int)blockIdx.z * GP + g, G - 1);   // (a group's last heads again, where there are fewer)
-    Piece<T>::get(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)b * a.q_ld + head[g] * DH + c * N), q[g]);
-    m[g] = -INFINITY;
-    l[g] = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      q[g][i] *= a.scale2;
-      acc[g][i] = 0.f;
-    }
-  }
-  const int32_t* const table = a.table + (size_t)b * a.cols;
-  for (int t0 = wave * TPW; t0 < held; t0 += kWaves * TPW) {
-    const int t = t0 + group;
-    bool open = t < held;
-    size_t slot = 0;
-    if (open) {
-      const int p = first + t, id = table[ring_column(p >> a.page_bits, a.cols)];
-      if ((unsigned)id >= (unsigned)a.n_pages) {
-        *a.err_flag = 1;
-        open = false;
-      } else {
-        slot = ((size_t)id << a.page_bits) + (p & ((1 << a.page_bits) - 1));
-        if (a.mask && a.mask[slot] == 0) open = false;
-      }
-    }
-    uint4 kp = make_uint4(0, 0, 0, 0), vp = kp;
-    if (open) {
-      kp = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.k) + slot * a.k_ld + kh * DH + c * N);
-      vp = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + slot * a.v_ld + kh * DH + c * N);
-    }
-    float k[N], v[N];
-    Piece<T>::get(kp, k);
-    Piece<T>::get(vp, v);
-#pragma unroll
-    for (int g = 0; g < GP; ++g) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) s = fmaf(q[g][i], k[i], s);
-#pragma unroll
-      for (int o = 1; o < LPH; o <<= 1) s += __shfl_xor(s, o);
-      if (!open) s = -INFINITY;
-      const float top = fmaxf(m[g], s), ref = top == -INFINITY ? 0.f : top;
-      const float keep = __builtin_amdgcn_exp2f(m[g] - ref), w = __builtin_amdgcn_exp2f(s - ref);
-      m[g] = top;
-      l[g] = fmaf(l[g], keep, w);
-#pragma unroll
-      for (int i = 0; i < N; ++i) acc[g][i] = fmaf(acc[g][i], keep, w * v[i]);
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < GP; ++g) {
-    if (c == 0) {
-      s_m[wave][group][g] = m[g];
-      s_l[wave][group][g] = l[g];
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) s_o[wave][group][g][c * N + i] = acc[g][i];
-  }
+  for (int b = b0; b < b1; ++b) s_units[b] += base;
+  if (tid == 0) s_units[B] = total;
   __syncthreads();
-  for (int i = tid; i < GP * LPH; i += kThreads) {
-    const int g = i / LPH, cc = i % LPH;
-    if ((int)blockIdx.z * GP + g >= G) continue;
-    float top = -INFINITY, sum = 0.f, row[N] = {};
-    for (int w = 0; w < kWaves; ++w)
-      for (int j = 0; j < TPW; ++j) top = fmaxf(top, s_m[w][j][g]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    for (int w = 0; w < kWaves; ++w)
-      for (int j = 0; j < TPW; ++j) {
-        const float f = __builtin_amdgcn_exp2f(s_m[w][j][g] - ref);
-        sum = fmaf(s_l[w][j][g], f, sum);
-#pragma unroll
-        for (int e = 0; e < N; ++e) row[e] = fmaf(s_o[w][j][g][cc * N + e], f, row[e]);
+
+  // rows of streams that hold nothing
+  for (int b = blockIdx.x; b < B; b += gridDim.x)
+    if (s_units[b + 1] == s_units[b])
+      for (int i = tid; i < a.heads * DH / 4; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
+
+  const int passes = (G + Core::kGroup - 1) / Core::kGroup, slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
+  const int WS = a.wave_slabs, TS = NW / WS, slab_groups = (slabs + WS - 1) / WS;
+  const int range = blockIdx.x / slab_groups, slab_group = blockIdx.x - range * slab_groups;
+  // (a tile a wavefront at least)
+  const int ranges = max(1, min(a.ranges, (total + TS - 1) / TS));
+  if (range >= ranges) return;
+  const int begin = (int)((int64_t)total * range / ranges), end = (int)((int64_t)total * (range + 1) / ranges);
+  if (begin >= end) return;
+  unsigned char* const lds = smem + wave * Core::kBytes;
+  const int my_slab = slab_group * WS + wave % WS, my_part = wave / WS;
+  for (int b = uniform(stream_of(s_units, B, begin)); b < B; ++b) {
+    const int u_first = uniform(s_units[b]), u_all = uniform(s_units[b + 1]) - u_first;
+    if (u_first >= end) break;
+    if (u_all == 0) continue;
+    const int u0 = max(begin - u_first, 0), u1 = min(end - u_first, u_all);
+    const int first = uniform(a.span[b].x), behind = first + uniform(a.span[b].y);
+    if (my_slab < slabs) Core::run(a, lds, b, my_slab / passes, my_slab % passes, u0 + my_part, TS, u1, first, behind);
+    __syncthreads();
+    // the wavefronts' rows of a query head to one maximum, and added
+    const bool whole = u1 - u0 == u_all;
+    const size_t place = ((size_t)range * 2 + (u0 == 0 && begin < u_first ? 1 : 0)) * a.heads;
+    for (int i = tid; i < WS * Core::kRows * (DH / 4); i += kThreads) {
+      const int quad = i % (DH / 4), row = i / (DH / 4) % Core::kRows, w = i / (DH / 4) / Core::kRows;
+      const int s = slab_group * WS + w, kh = s / passes * Core::kSlabHeads + row / Core::kGroup, in_group = s % passes * Core::kGroup + row % Core::kGroup;
+      if (s >= slabs || kh >= a.kv_heads || in_group >= G) continue;
+      const int head = kh * G + in_group;
+      float top = -INFINITY, l = 0.f;
+      for (int p = 0; p < TS; ++p) top = fmaxf(top, reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes)->m[row]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int p = 0; p < TS; ++p) {
+        const Result* const r = reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes);
+        const float f = __builtin_amdgcn_exp2f(r->m[row] - ref);
+        const float4 v = *reinterpret_cast<const float4*>(&r->o[row][4 * quad]);
+        l = fmaf(r->l[row], f, l);
+        o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
       }
-    const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+      if (whole) {
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
+        store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      } else {
+        if (quad == 0) put2(a.partial_ml + place + head, make_float2(top, l));
+        float2* const row = reinterpret_cast<float2*>(a.partial + (place + head) * DH + 4 * quad);
+        put2(row, make_float2(o.x, o.y));
+        put2(row + 1, make_float2(o.z, o.w));
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // (a piece has arrived in memory before its workgroup is counted)
+    __syncthreads();   // the LDS is the next stream's, or the pieces'
+    if (whole) continue;
+    // The pieces of a stream: the workgroup that ends last adds them up, in the order of the ranges.
+    const int r0 = (int)((((int64_t)u_first + 1) * ranges - 1) / total), r1 = (int)(((int64_t)(u_first + u_all) * ranges - 1) / total);
+    if (tid == 0) {
+      int32_t* const ticket = a.tickets + (size_t)b * slab_groups + slab_group;
+      s_flag = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == r1 - r0;
+      if (s_flag) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!s_flag) continue;
+    const bool inside = (int)((int64_t)total * r0 / ranges) < u_first;   // the first piece does not begin with its range
+    // the group's query heads, one behind the other; as many threads a quad of columns as there are
+    const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
+    const int items = heads * (DH / 4), parts = max(1, kThreads / items);
+    Sum* const s_sum = reinterpret_cast<Sum*>(smem);
+    for (int i0 = 0; i0 < items; i0 += kThreads) {
+      const int item = i0 + (parts > 1 ? tid % items : tid), part = parts > 1 ? tid / items : 0;
+      const int head = head0 + item / (DH / 4), quad = item % (DH / 4);
+      Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      if (item < items && part < parts) {
+        // (four at a time: loads of device scope are not moved past what is done with the one before)
+        constexpr int N = 4;
+        for (int r = r0 + part; r <= r1; r += N * parts) {
+          float2 ml[N], lo[N], hi[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) row[e] *= inv;
-    *reinterpret_cast<uint4*>(static_cast<T*>(a.out) + (size_t)b * a.out_ld + (kh * G + blockIdx.z * GP + g) * DH + cc * N) = Piece<T>::put(row);
+          for (int n = 0; n < N; ++n) {
+            const int piece = min(r + n * parts, r1);
+            const size_t at = ((size_t)piece * 2 + (piece == r0 && inside ? 1 : 0)) * a.heads + head;
+            const float2* const row = reinterpret_cast<const float2*>(a.partial + at * DH + 4 * quad);
+            ml[n] = get2(a.partial_ml + at);
+            lo[n] = get2(row);
+            hi[n] = get2(row + 1);
+          }
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            if (r + n * parts <= r1) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
+        }
+      }
+      if (parts > 1) {
+        s_sum[tid] = sum;
+        __syncthreads();
+        if (part == 0)
+          for (int p = 1; p < parts; ++p) sum.add(s_sum[p * items + tid]);
+      }
+      if (item < items && part == 0) {
+        const float inv = sum.l != 0.f ? 1.0f / sum.l : 0.f;
+        store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad, make_float4(sum.o.x * inv, sum.o.y * inv, sum.o.z * inv, sum.o.w * inv));
+      }
+    }
+    __syncthreads();
   }
 }
 
-template <typename T, int DH>
-hipError_t launch(const MemoryAttentionArgs& a, hipStream_t s) {
-  const int G = a.heads / a.kv_heads;
-  if (G == 1)
-    hipLaunchKernelGGL((memory_attention_kernel<T, DH, 1>), dim3(a.B, a.kv_heads, 1), dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((memory_attention_kernel<T, DH, 2>), dim3(a.B, a.kv_heads, (G + 1) / 2), dim3(kThreads), 0, s, a);
+template <typename Core, int DH, int NW>
+hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
+  const int G = a.heads / a.kv_heads, passes = (G + Core::kGroup - 1) / Core::kGroup;
+  const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
+  a.wave_slabs = slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
+  const int slab_groups = slabs / a.wave_slabs;
+  a.ranges = std::max(1, 2 * cus / slab_groups);
+  const size_t lds = kLds<Core, NW> + (size_t)(a.B + 1) * sizeof(int);
+  static DeviceOnce once;
+  if (hipError_t e = allow_lds(memory_attention_kernel<Core, DH, NW>, kLds<Core, NW> + (kMemoryMaxStreams + 1) * sizeof(int), &once); e != hipSuccess) return e;
+  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3(a.ranges * slab_groups), dim3(64 * NW), lds, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, hipStream_t s) {
-  if (d_head == 64) return use_bf16 ? launch<bf16_t, 64>(a, s) : launch<float, 64>(a, s);
-  if (d_head == 32) return use_bf16 ? launch<bf16_t, 32>(a, s) : launch<float, 32>(a, s);
+MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
+  // (as many ranges as there may be, two pieces each; slabs are query heads at most)
+  const uint64_t pieces = (uint64_t)2 * 2 * cus * heads;
+  return {pieces * sizeof(float2), pieces * d_head * sizeof(float), (uint64_t)max_streams * heads * sizeof(int32_t)};
+}
+
+hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, int cus, hipStream_t s) {
+  if (d_head == 64) return use_bf16 ? launch<Core16<64>, 64, 8>(a, cus, s) : launch<Core32<64>, 64, 8>(a, cus, s);
+  if (d_head == 32) return use_bf16 ? launch<Core16<32>, 32, 8>(a, cus, s) : launch<Core32<32>, 32, 8>(a, cus, s);
   return hipErrorInvalidValue;
 }
 
