@@ -548,7 +548,7 @@ struct MemoryAttentionArgs {
   float* partial;
   int32_t* tickets;
   const void* zeros;
-  int ranges, wave_slabs;   // the launcher's
+  int places, wave_slabs;   // the launcher's
 };
 struct MemoryAttentionSpace {
   uint64_t ml, rows, tickets;   // bytes

@@ -4,11 +4,11 @@
 // One pass over keys and values, with a running maximum and sum.  Every key and value is read once for the G query
 // heads that share it: 2 G operations a byte in bf16, so memory bounds it.
 //
-// The tokens of all streams are one row of units of 32 positions, cut into ranges of one length, a workgroup each (lengths are
-// known on the device only, so every workgroup adds the streams' units up for itself).  A range may end inside a stream and
-// hold several: every piece of a stream gives a row under its own maximum; a stream that lies in one range is
-// finished there, the pieces of the others go to memory and the workgroup that ends last adds them up in order.
-// Units lie on multiples of 32 positions and pages hold 8 or more, so eight consecutive tokens of a unit are in one page.
+// A stream's tokens are units of 32 positions, cut into pieces of one length for all streams, a workgroup each (lengths are
+// known on the device only, so every workgroup works the cut out for itself).  A piece gives a row under its own maximum; a
+// stream of one piece is finished there, the rows of the others go to memory and the workgroup that ends last adds
+// them up in order.  Units lie on multiples of 32 positions and pages hold 8 or more, so eight consecutive tokens of
+// a unit are in one page.
 #include <algorithm>
 #include <type_traits>
 
@@ -20,6 +20,7 @@ namespace cfdetr {
 namespace {
 
 constexpr int kUnit = 32;             // tokens
+constexpr int kLeast = 4;             // units a wavefront that a piece has at least
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -388,6 +389,11 @@ struct Sum {
     l = fmaf(l, f, s.l * g);
     o = make_float4(fmaf(o.x, f, s.o.x * g), fmaf(o.y, f, s.o.y * g), fmaf(o.z, f, s.o.z * g), fmaf(o.w, f, s.o.w * g));
   }
+  template <typename T>
+  __device__ __forceinline__ void store(T* to) const {
+    const float inv = l != 0.f ? 1.0f / l : 0.f;
+    store4(to, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  }
 };
 // First query head of a slab: slabs go through the key heads and, where a key head has more query heads than a wavefront takes,
 // through groups of these, so that the query heads of consecutive slabs lie behind each other.
@@ -400,7 +406,7 @@ __device__ __forceinline__ int first_head(int slab, int passes, int G) {
 template <typename Core, int NW>
 constexpr int kLds = std::max(NW * Core::kBytes, 64 * NW * (int)sizeof(Sum));
 
-// Workgroup: one of `a.ranges` ranges of units and a.wave_slabs of the slabs; its NW wavefronts have one slab each, and where
+// Workgroup: one piece of a stream and a.wave_slabs of the slabs; its NW wavefronts have one slab each, and where
 // that leaves some over, every second, third, .. tile of it.
 template <typename Core, int DH, int NW>
 __global__ __launch_bounds__(64 * NW, 4) void memory_attention_kernel(MemoryAttentionArgs a) {
@@ -409,36 +415,37 @@ __global__ __launch_bounds__(64 * NW, 4) void memory_attention_kernel(MemoryAtte
   constexpr int kThreads = 64 * NW;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   __shared__ int s_wave[2][NW], s_flag;
-  int* const s_units = reinterpret_cast<int*>(smem + kLds<Core, NW>);   // [B + 1] exclusive sums of the streams' units
+  int* const s_piece = reinterpret_cast<int*>(smem + kLds<Core, NW>);   // [B + 1] pieces of the streams before
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = uniform(tid >> 6);
   const int B = a.B, G = a.heads / a.kv_heads;
 
-  // units of every stream, and their sums
+  // units of all streams
   if (tid == 0) s_flag = 0;
   __syncthreads();
   const int per = (B + kThreads - 1) / kThreads, b0 = tid * per, b1 = min(B, b0 + per);
+  auto units_of = [](int2 span) { return span.y > 0 ? (span.x + span.y - 1) / kUnit - span.x / kUnit + 1 : 0; };
   int mine = 0;
   bool bad = false;
   for (int b = b0; b < b1; ++b) {
     const int2 span = a.span[b];
     const bool wrong = span_is_bad(span.x, span.y, a.page_bits, a.cols);
-    s_units[b] = mine;
     bad |= wrong;
-    if (!wrong && span.y > 0) mine += ((span.x + span.y - 1) / kUnit) - span.x / kUnit + 1;
+    const int units = wrong ? 0 : units_of(span);
+    s_piece[b] = units;
+    mine += units;
   }
   if (bad) s_flag = 1;
   // (a thread's units are below 2^28; their thousands tell whether the sum fits 32 bits)
-  const int upto = sum_upto(mine), thousands = sum_upto((mine + 1023) / 1024);
+  const int upto_all = sum_upto(mine), thousands = sum_upto((mine + 1023) / 1024);
   if (lane == 63) {
-    s_wave[0][wave] = upto;
+    s_wave[0][wave] = upto_all;
     s_wave[1][wave] = thousands;
   }
   __syncthreads();
-  int base = upto - mine, total = 0, all_thousands = 0;
+  int total = 0, all_thousands = 0;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
-    if (w < wave) base += s_wave[0][w];
     total += s_wave[0][w];
     all_thousands += s_wave[1][w];
   }
@@ -447,114 +454,107 @@ __global__ __launch_bounds__(64 * NW, 4) void memory_attention_kernel(MemoryAtte
     if (blockIdx.x == 0 && tid == 0) *a.err_flag = 1;
     return;
   }
-  for (int b = b0; b < b1; ++b) s_units[b] += base;
-  if (tid == 0) s_units[B] = total;
+  // the pieces' length, and how many there are of every stream: each stream's last one is shorter, so a piece a stream is left over
+  const int passes = (G + Core::kGroup - 1) / Core::kGroup, slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
+  const int WS = a.wave_slabs, TS = NW / WS, slab_groups = slabs / WS;
+  const int room = max(a.places / 2, a.places - B), length = max(kLeast * TS, (total + room - 1) / room);
+  mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int pieces = (s_piece[b] + length - 1) / length;
+    s_piece[b] = mine;
+    mine += pieces;
+  }
+  const int upto = sum_upto(mine);
+  __syncthreads();
+  if (lane == 63) s_wave[0][wave] = upto;
+  __syncthreads();
+  int base = upto - mine;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) base += w < wave ? s_wave[0][w] : 0;
+  for (int b = b0; b < b1; ++b) s_piece[b] += base;
+  if (tid == kThreads - 1) s_piece[B] = base + mine;
   __syncthreads();
 
   // rows of streams that hold nothing
   for (int b = blockIdx.x; b < B; b += gridDim.x)
-    if (s_units[b + 1] == s_units[b])
+    if (s_piece[b + 1] == s_piece[b])
       for (int i = tid; i < a.heads * DH / 4; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
 
-  const int passes = (G + Core::kGroup - 1) / Core::kGroup, slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
-  const int WS = a.wave_slabs, TS = NW / WS, slab_groups = (slabs + WS - 1) / WS;
-  const int range = blockIdx.x / slab_groups, slab_group = blockIdx.x - range * slab_groups;
-  // (a tile a wavefront at least)
-  const int ranges = max(1, min(a.ranges, (total + TS - 1) / TS));
-  if (range >= ranges) return;
-  const int begin = (int)((int64_t)total * range / ranges), end = (int)((int64_t)total * (range + 1) / ranges);
-  if (begin >= end) return;
-  unsigned char* const lds = smem + wave * Core::kBytes;
-  const int my_slab = slab_group * WS + wave % WS, my_part = wave / WS;
-  for (int b = uniform(stream_of(s_units, B, begin)); b < B; ++b) {
-    const int u_first = uniform(s_units[b]), u_all = uniform(s_units[b + 1]) - u_first;
-    if (u_first >= end) break;
-    if (u_all == 0) continue;
-    const int u0 = max(begin - u_first, 0), u1 = min(end - u_first, u_all);
-    const int first = uniform(a.span[b].x), behind = first + uniform(a.span[b].y);
-    if (my_slab < slabs) Core::run(a, lds, b, my_slab / passes, my_slab % passes, u0 + my_part, TS, u1, first, behind);
-    __syncthreads();
-    // the wavefronts' rows of a query head to one maximum, and added
-    const bool whole = u1 - u0 == u_all;
-    const size_t place = ((size_t)range * 2 + (u0 == 0 && begin < u_first ? 1 : 0)) * a.heads;
-    for (int i = tid; i < WS * Core::kRows * (DH / 4); i += kThreads) {
-      const int quad = i % (DH / 4), row = i / (DH / 4) % Core::kRows, w = i / (DH / 4) / Core::kRows;
-      const int s = slab_group * WS + w, kh = s / passes * Core::kSlabHeads + row / Core::kGroup, in_group = s % passes * Core::kGroup + row % Core::kGroup;
-      if (s >= slabs || kh >= a.kv_heads || in_group >= G) continue;
-      const int head = kh * G + in_group;
-      float top = -INFINITY, l = 0.f;
-      for (int p = 0; p < TS; ++p) top = fmaxf(top, reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes)->m[row]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int p = 0; p < TS; ++p) {
-        const Result* const r = reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes);
-        const float f = __builtin_amdgcn_exp2f(r->m[row] - ref);
-        const float4 v = *reinterpret_cast<const float4*>(&r->o[row][4 * quad]);
-        l = fmaf(r->l[row], f, l);
-        o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
-      }
-      if (whole) {
-        const float inv = l != 0.f ? 1.0f / l : 0.f;
-        store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-      } else {
-        if (quad == 0) put2(a.partial_ml + place + head, make_float2(top, l));
-        float2* const row = reinterpret_cast<float2*>(a.partial + (place + head) * DH + 4 * quad);
-        put2(row, make_float2(o.x, o.y));
-        put2(row + 1, make_float2(o.z, o.w));
-      }
+  const int piece = blockIdx.x / slab_groups, slab_group = blockIdx.x - piece * slab_groups;
+  if (piece >= s_piece[B]) return;
+  const int b = uniform(stream_of(s_piece, B, piece));
+  const int piece0 = uniform(s_piece[b]), pieces = uniform(s_piece[b + 1]) - piece0;
+  const int first = uniform(a.span[b].x), held = uniform(a.span[b].y);
+  const int u0 = (piece - piece0) * length, u1 = min(u0 + length, units_of(make_int2(first, held)));
+  const int my_slab = slab_group * WS + wave % WS;
+  Core::run(a, smem + wave * Core::kBytes, b, my_slab / passes, my_slab % passes, u0 + wave / WS, TS, u1, first, first + held);
+  __syncthreads();
+
+  // the wavefronts' rows of a query head to one maximum, and added
+  for (int i = tid; i < WS * Core::kRows * (DH / 4); i += kThreads) {
+    const int quad = i % (DH / 4), row = i / (DH / 4) % Core::kRows, w = i / (DH / 4) / Core::kRows;
+    const int s = slab_group * WS + w, kh = s / passes * Core::kSlabHeads + row / Core::kGroup, in_group = s % passes * Core::kGroup + row % Core::kGroup;
+    if (kh >= a.kv_heads || in_group >= G) continue;
+    const int head = kh * G + in_group;
+    Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int p = 0; p < TS; ++p) {
+      const Result* const r = reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes);
+      sum.add(Sum{r->m[row], r->l[row], *reinterpret_cast<const float4*>(&r->o[row][4 * quad])});
     }
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // (a piece has arrived in memory before its workgroup is counted)
-    __syncthreads();   // the LDS is the next stream's, or the pieces'
-    if (whole) continue;
-    // The pieces of a stream: the workgroup that ends last adds them up, in the order of the ranges.
-    const int r0 = (int)((((int64_t)u_first + 1) * ranges - 1) / total), r1 = (int)(((int64_t)(u_first + u_all) * ranges - 1) / total);
-    if (tid == 0) {
-      int32_t* const ticket = a.tickets + (size_t)b * slab_groups + slab_group;
-      s_flag = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == r1 - r0;
-      if (s_flag) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (pieces == 1) {
+      sum.store(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad);
+    } else {
+      const size_t at = (size_t)piece * a.heads + head;
+      if (quad == 0) put2(a.partial_ml + at, make_float2(sum.m, sum.l));
+      float2* const to = reinterpret_cast<float2*>(a.partial + at * DH + 4 * quad);
+      put2(to, make_float2(sum.o.x, sum.o.y));
+      put2(to + 1, make_float2(sum.o.z, sum.o.w));
     }
-    __syncthreads();
-    if (!s_flag) continue;
-    const bool inside = (int)((int64_t)total * r0 / ranges) < u_first;   // the first piece does not begin with its range
-    // the group's query heads, one behind the other; as many threads a quad of columns as there are
-    const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
-    const int items = heads * (DH / 4), parts = max(1, kThreads / items);
-    Sum* const s_sum = reinterpret_cast<Sum*>(smem);
-    for (int i0 = 0; i0 < items; i0 += kThreads) {
-      const int item = i0 + (parts > 1 ? tid % items : tid), part = parts > 1 ? tid / items : 0;
-      const int head = head0 + item / (DH / 4), quad = item % (DH / 4);
-      Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-      if (item < items && part < parts) {
-        // (four at a time: loads of device scope are not moved past what is done with the one before)
-        constexpr int N = 4;
-        for (int r = r0 + part; r <= r1; r += N * parts) {
-          float2 ml[N], lo[N], hi[N];
+  }
+  if (pieces == 1) return;
+  // the pieces of a stream: the workgroup that ends last adds them up, in order
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // (a piece has arrived in memory before its workgroup is counted)
+  __syncthreads();
+  if (tid == 0) {
+    int32_t* const ticket = a.tickets + (size_t)b * slab_groups + slab_group;
+    s_flag = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
+    if (s_flag) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!s_flag) return;
+  // the group's query heads, one behind the other; as many threads a quad of columns as there are
+  const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
+  const int items = heads * (DH / 4), parts = max(1, kThreads / items);
+  Sum* const s_sum = reinterpret_cast<Sum*>(smem);
+  for (int i0 = 0; i0 < items; i0 += kThreads) {
+    const int item = i0 + (parts > 1 ? tid % items : tid), part = parts > 1 ? tid / items : 0;
+    const int head = head0 + item / (DH / 4), quad = item % (DH / 4);
+    Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    if (item < items && part < parts) {
+      // (four at a time: loads of device scope are not moved past what is done with the one before)
+      constexpr int N = 4;
+      for (int r = part; r < pieces; r += N * parts) {
+        float2 ml[N], lo[N], hi[N];
 #pragma unroll
-          for (int n = 0; n < N; ++n) {
-            const int piece = min(r + n * parts, r1);
-            const size_t at = ((size_t)piece * 2 + (piece == r0 && inside ? 1 : 0)) * a.heads + head;
-            const float2* const row = reinterpret_cast<const float2*>(a.partial + at * DH + 4 * quad);
-            ml[n] = get2(a.partial_ml + at);
-            lo[n] = get2(row);
-            hi[n] = get2(row + 1);
-          }
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-            if (r + n * parts <= r1) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
+        for (int n = 0; n < N; ++n) {
+          const size_t at = (size_t)(piece0 + min(r + n * parts, pieces - 1)) * a.heads + head;
+          const float2* const from = reinterpret_cast<const float2*>(a.partial + at * DH + 4 * quad);
+          ml[n] = get2(a.partial_ml + at);
+          lo[n] = get2(from);
+          hi[n] = get2(from + 1);
         }
-      }
-      if (parts > 1) {
-        s_sum[tid] = sum;
-        __syncthreads();
-        if (part == 0)
-          for (int p = 1; p < parts; ++p) sum.add(s_sum[p * items + tid]);
-      }
-      if (item < items && part == 0) {
-        const float inv = sum.l != 0.f ? 1.0f / sum.l : 0.f;
-        store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad, make_float4(sum.o.x * inv, sum.o.y * inv, sum.o.z * inv, sum.o.w * inv));
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (r + n * parts < pieces) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
       }
     }
-    __syncthreads();
+    if (parts > 1) {
+      s_sum[tid] = sum;
+      __syncthreads();
+      if (part == 0)
+        for (int p = 1; p < parts; ++p) sum.add(s_sum[p * items + tid]);
+    }
+    if (item < items && part == 0) sum.store(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad);
   }
 }
 
@@ -564,19 +564,19 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
   a.wave_slabs = slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
-  a.ranges = std::max(1, 2 * cus / slab_groups);
+  a.places = std::max(1, 2 * cus / slab_groups);
   const size_t lds = kLds<Core, NW> + (size_t)(a.B + 1) * sizeof(int);
   static DeviceOnce once;
   if (hipError_t e = allow_lds(memory_attention_kernel<Core, DH, NW>, kLds<Core, NW> + (kMemoryMaxStreams + 1) * sizeof(int), &once); e != hipSuccess) return e;
-  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3(a.ranges * slab_groups), dim3(64 * NW), lds, s, a);
+  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), lds, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
-  // (as many ranges as there may be, two pieces each; slabs are query heads at most)
-  const uint64_t pieces = (uint64_t)2 * 2 * cus * heads;
+  // (slabs are query heads at most)
+  const uint64_t pieces = (uint64_t)(2 * cus + max_streams) * heads;
   return {pieces * sizeof(float2), pieces * d_head * sizeof(float), (uint64_t)max_streams * heads * sizeof(int32_t)};
 }
 
