@@ -21,6 +21,8 @@ namespace {
 
 constexpr int kUnit = 32;             // tokens
 constexpr int kLeast = 4;             // units a wavefront that a piece has at least
+constexpr int kWaves = 4, kDepth = 2; // wavefronts of a workgroup, tiles that each has asked for
+constexpr int kPlaces = 2;            // workgroups a CU at once, for which streams are cut and pieces have room in memory
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -90,13 +92,14 @@ struct Rows {
 // Logits are products of 16 tokens x 32 features x 16 query heads, S^T = K Q^T, which leave lane l query head l mod 16 and tokens
 // 4 (l / 16) + r of either half of the tile; these are at once the operand of O^T = V^T P^T if the products' index runs over
 // the tokens in that order, so weights never leave their lane.  With one query head of 16 the products are 15 parts zeros and still cost a
-// fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own; keys of the next tile are asked
-// for when the logits are taken, values when the row is: no barrier in the loop.
-template <int DH>
+// fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own, DEPTH tiles ahead: no barrier in
+// the loop.
+template <int DH, int DEPTH>
 struct Core16 {
   typedef bf16_t T;
   static constexpr int kSlabHeads = 64 / DH, kGroup = 16, kRows = kSlabHeads * kGroup;
-  static constexpr int kBytes = 2 * kUnit * 128;   // LDS: keys, values
+  static constexpr int kTile = 2 * kUnit * 128;    // LDS of a tile: keys, values
+  static constexpr int kBytes = DEPTH * kTile;
   typedef Rows<kRows, DH> Result;
   static_assert(sizeof(Result) <= kBytes, "in place of keys and values");
 
@@ -135,9 +138,7 @@ struct Core16 {
     const uint32_t k_lane = (uint32_t)(lane >> 3) * k_step + slab * 128, v_lane = (uint32_t)(lane >> 3) * v_step + slab * 128;
     const uint32_t k_even = k_lane + (half ? kc & 3 : kc) * 16, k_odd = k_lane + (half ? kc & 3 : kc ^ 4) * 16;
     const uint32_t v_off = v_lane + (half ? vc & 3 : vc) * 16;
-    unsigned char* const sK = lds;
-    unsigned char* const sV = lds + kUnit * 128;
-    const uint32_t ldsK = (uint32_t)(uintptr_t)sK, ldsV = ldsK + kUnit * 128;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int p_first = first & ~(kUnit - 1), page_mask = (1 << a.page_bits) - 1;
 
 #pragma nounroll
@@ -152,46 +153,86 @@ struct Core16 {
 #pragma unroll
         for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[h][s].x), "+v"(qf[h][s].y), "+v"(qf[h][s].z), "+v"(qf[h][s].w));
 
-      auto load = [&](const void* base, uint32_t row, uint32_t even, uint32_t odd, int i, uint32_t to) {
+      auto load = [&](int i, uint32_t to) {
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
         const int p0 = p_first + (unit + i * step) * kUnit;
+        const char *k[4], *v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int id = __builtin_amdgcn_readlane(t.id[j], i);
           const size_t slot = ((size_t)id << a.page_bits) + ((p0 + 8 * j) & page_mask);
-          const char* const from = static_cast<const char*>(base) + slot * row;
-          const uint32_t off = j & 1 ? odd : even;
-          if (open == 0xFFFFFFFFu) {
-            dma16(from, off, to + j * 1024);
-          } else {
-            // tokens that are not read: zeros, from the one place that all such lanes share
-            const bool read = open >> (8 * j + (lane >> 3)) & 1;
-            dma16(read ? from + off : static_cast<const char*>(a.zeros), to + j * 1024);
-          }
+          k[j] = static_cast<const char*>(a.k) + slot * k_step;
+          v[j] = static_cast<const char*>(a.v) + slot * v_step;
+        }
+        if (open == 0xFFFFFFFFu) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dma16(k[j], j & 1 ? k_odd : k_even, to + j * 1024);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dma16(v[j], v_off, to + (4 + j) * 1024);
+        } else {
+          // tokens that are not read: zeros, from the one place that all such lanes share
+          const char* const zeros = static_cast<const char*>(a.zeros);
+          const uint32_t mine = open >> (lane >> 3);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? k[j] + (j & 1 ? k_odd : k_even) : zeros, to + j * 1024);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? v[j] + v_off : zeros, to + (4 + j) * 1024);
         }
       };
-      load(a.k, k_step, k_even, k_odd, 0, ldsK);
-      load(a.v, v_step, v_off, v_off, 0, ldsV);
+      for (int i = 0; i < min(DEPTH, count); ++i) load(i, lds0 + i * kTile);
+      int place = 0;
 #pragma nounroll
       for (int i = 0; i < count; ++i) {
-        const bool more = i + 1 < count;
-        asm volatile("s_waitcnt vmcnt(4)" : : : "memory");   // the keys; their values need not be there yet
+        // this tile's eight loads; those of the tiles behind it need not be there yet
+        const int behind = min(DEPTH, count - i) - 1;
+        if (behind == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        else if (behind == 1) asm volatile("s_waitcnt vmcnt(8)" : : : "memory");
+        else if (behind == 2) asm volatile("s_waitcnt vmcnt(16)" : : : "memory");
+        else asm volatile("s_waitcnt vmcnt(24)" : : : "memory");
+        static_assert(DEPTH <= 4, "the counts above");
+        const unsigned char* const sK = lds + place;
+        const unsigned char* const sV = sK + kUnit * 128;
+        // all operands at once: the tile's place is free for the next loads before a product is taken, and no product waits for a read
+        typedef __attribute__((ext_vector_type(4))) short s16x4;
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        bf16x8 kf[NH][2][KS];
+        union {
+          s16x4 part[2];
+          bf16x8 whole;
+        } v[NH][NB];
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int half16 = 0; half16 < 2; ++half16)
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+              const int row = 16 * half16 + l16, piece = (h * KS + c) * 4 + g;
+              kf[h][half16][c] = *reinterpret_cast<const bf16x8*>(sK + row * 128 + (piece ^ ((row >> 1) & 7)) * 16);
+            }
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int half16 = 0; half16 < 2; ++half16) {
+              // the transposing read gives a lane four tokens of its column, 16 lanes naming the pieces of four tokens by 16 columns
+              const int row = 16 * half16 + 4 * g + (l16 >> 2);
+              v[h][n].part[half16] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(
+                  sV + row * 128 + ((h * NB + n) ^ ((row >> 1) & 3)) * 32 + (lane & 3) * 8));
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        if (i + DEPTH < count) load(i + DEPTH, lds0 + place);
+        place = place + kTile == kBytes ? 0 : place + kTile;
         f32x4 s[NH][2];
 #pragma unroll
         for (int h = 0; h < NH; ++h)
 #pragma unroll
           for (int half16 = 0; half16 < 2; ++half16) {
-            const int row = 16 * half16 + l16;
             s[h][half16] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < KS; ++c) {
-              const int piece = (h * KS + c) * 4 + g;
-              const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sK + row * 128 + (piece ^ ((row >> 1) & 7)) * 16);
-              s[h][half16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, *reinterpret_cast<const bf16x8*>(&qf[h][c]), s[h][half16], 0, 0, 0);
-            }
+            for (int c = 0; c < KS; ++c)
+              s[h][half16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][half16][c], *reinterpret_cast<const bf16x8*>(&qf[h][c]), s[h][half16], 0, 0, 0);
           }
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-        if (more) load(a.k, k_step, k_even, k_odd, i + 1, ldsK);
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
         bf16x8 w[NH];
 #pragma unroll
@@ -228,29 +269,10 @@ struct Core16 {
           const uint4 packed = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
           w[h] = *reinterpret_cast<const bf16x8*>(&packed);
         }
-        if (more) asm volatile("s_waitcnt vmcnt(4)" : : : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        typedef __attribute__((ext_vector_type(4))) short s16x4;
-        typedef __attribute__((address_space(3))) s16x4* lds4;
 #pragma unroll
         for (int h = 0; h < NH; ++h)
 #pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            // the transposing read gives a lane four tokens of its column, 16 lanes naming the pieces of four tokens by 16 columns
-            union {
-              s16x4 part[2];
-              bf16x8 whole;
-            } v;
-#pragma unroll
-            for (int half16 = 0; half16 < 2; ++half16) {
-              const int row = 16 * half16 + 4 * g + (l16 >> 2);
-              v.part[half16] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (lds4)(sV + row * 128 + ((h * NB + n) ^ ((row >> 1) & 3)) * 32 + (lane & 3) * 8));
-            }
-            acc[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.whole, w[h], acc[h][n], 0, 0, 0);
-          }
-        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-        if (more) load(a.v, v_step, v_off, v_off, i + 1, ldsV);
+          for (int n = 0; n < NB; ++n) acc[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h][n].whole, w[h], acc[h][n], 0, 0, 0);
       }
     }
     // (the LDS of keys and values is free: every read has been waited for)
@@ -409,7 +431,7 @@ constexpr int kLds = std::max(NW * Core::kBytes, 64 * NW * (int)sizeof(Sum));
 // Workgroup: one piece of a stream and a.wave_slabs of the slabs; its NW wavefronts have one slab each, and where
 // that leaves some over, every second, third, .. tile of it.
 template <typename Core, int DH, int NW>
-__global__ __launch_bounds__(64 * NW, 4) void memory_attention_kernel(MemoryAttentionArgs a) {
+__global__ __launch_bounds__(64 * NW, kPlaces * NW / 4) void memory_attention_kernel(MemoryAttentionArgs a) {
   typedef typename Core::T T;
   typedef typename Core::Result Result;
   constexpr int kThreads = 64 * NW;
@@ -562,9 +584,9 @@ template <typename Core, int DH, int NW>
 hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   const int G = a.heads / a.kv_heads, passes = (G + Core::kGroup - 1) / Core::kGroup;
   const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
-  a.wave_slabs = slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
+  a.wave_slabs = NW % 4 == 0 && slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
-  a.places = std::max(1, 2 * cus / slab_groups);
+  a.places = std::max(1, kPlaces * cus / slab_groups);
   const size_t lds = kLds<Core, NW> + (size_t)(a.B + 1) * sizeof(int);
   static DeviceOnce once;
   if (hipError_t e = allow_lds(memory_attention_kernel<Core, DH, NW>, kLds<Core, NW> + (kMemoryMaxStreams + 1) * sizeof(int), &once); e != hipSuccess) return e;
@@ -575,14 +597,14 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
 }  // namespace
 
 MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
-  // (slabs are query heads at most)
-  const uint64_t pieces = (uint64_t)(2 * cus + max_streams) * heads;
+  // (as many pieces as places and streams, and slabs as query heads, at most)
+  const uint64_t pieces = (uint64_t)(kPlaces * cus + max_streams) * heads;
   return {pieces * sizeof(float2), pieces * d_head * sizeof(float), (uint64_t)max_streams * heads * sizeof(int32_t)};
 }
 
 hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, int cus, hipStream_t s) {
-  if (d_head == 64) return use_bf16 ? launch<Core16<64>, 64, 8>(a, cus, s) : launch<Core32<64>, 64, 8>(a, cus, s);
-  if (d_head == 32) return use_bf16 ? launch<Core16<32>, 32, 8>(a, cus, s) : launch<Core32<32>, 32, 8>(a, cus, s);
+  if (d_head == 64) return use_bf16 ? launch<Core16<64, kDepth>, 64, kWaves>(a, cus, s) : launch<Core32<64>, 64, kWaves>(a, cus, s);
+  if (d_head == 32) return use_bf16 ? launch<Core16<32, kDepth>, 32, kWaves>(a, cus, s) : launch<Core32<32>, 32, kWaves>(a, cus, s);
   return hipErrorInvalidValue;
 }
 
