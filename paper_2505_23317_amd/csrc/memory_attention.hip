@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kUnit = 32;             // tokens
 constexpr int kLeast = 4;             // units a wavefront that a piece has at least
-constexpr int kWaves = 4, kDepth = 2; // wavefronts of a workgroup, tiles that each has asked for
+constexpr int kWaves = 8, kDepth = 1; // wavefronts of a workgroup, tiles that each has asked for
 constexpr int kPlaces = 2;            // workgroups a CU at once, for which streams are cut and pieces have room in memory
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -97,6 +97,7 @@ struct Rows {
 template <int DH, int DEPTH>
 struct Core16 {
   typedef bf16_t T;
+  static constexpr int kWavesSimd = kPlaces * kWaves / 4;
   static constexpr int kSlabHeads = 64 / DH, kGroup = 16, kRows = kSlabHeads * kGroup;
   static constexpr int kTile = 2 * kUnit * 128;    // LDS of a tile: keys, values
   static constexpr int kBytes = DEPTH * kTile;
@@ -297,6 +298,7 @@ struct Core16 {
 template <int DH>
 struct Core32 {
   typedef float T;
+  static constexpr int kWavesSimd = 2;
   static constexpr int kSlabHeads = 1, kGroup = 4, kRows = kGroup;
   typedef Rows<kRows, DH> Result;
   static constexpr int kBytes = (sizeof(Result) + 255) / 256 * 256;
@@ -424,142 +426,192 @@ __device__ __forceinline__ int first_head(int slab, int passes, int G) {
   return slab / passes * Core::kSlabHeads * G + slab % passes * Core::kGroup;
 }
 
-// LDS of a workgroup in front of the streams' units: the wavefronts', or the sums of a stream's pieces.
-template <typename Core, int NW>
-constexpr int kLds = std::max(NW * Core::kBytes, 64 * NW * (int)sizeof(Sum));
+// How the streams are cut, and which piece a workgroup has.
+struct Piece {
+  int stream, number, pieces;   // -1: there is no such piece
+  int length;                   // of all pieces but a stream's last, in units
+  int first, held;              // the stream's span
+  bool bad;                     // a span is none, or there are too many units
+};
+__device__ __forceinline__ int units_of(int2 span) { return span.y > 0 ? (span.x + span.y - 1) / kUnit - span.x / kUnit + 1 : 0; }
+// The wavefronts share the streams, rows of 64 that lie behind each other.  Up to 64 streams every wavefront has them all and needs no
+// barrier (one stream of 64 tokens 6.3 us, 7.2 with all three).
+template <int NW>
+__device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int piece, int least) {
+  constexpr int R = kMemoryMaxStreams / 64 / NW;   // rows of a wavefront, at most
+  __shared__ int s_sums[3][NW];
+  __shared__ Piece s_found;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), B = a.B;
+  const bool alone = B <= 64;
+  const int rows = alone ? 1 : (B + 64 * NW - 1) / (64 * NW), b0 = alone ? 0 : wave * rows * 64;
+  Piece p{-1, 0, 0, 0, 0, 0, false};
+  int2 span[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (r >= rows) break;
+    const int b = b0 + 64 * r + lane;
+    span[r] = b < B ? a.span[b] : make_int2(0, 0);
+  }
+  int units = 0;   // (of up to 8 streams of 2^24 units)
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (r >= rows) break;
+    if (span_is_bad(span[r].x, span[r].y, a.page_bits, a.cols)) p.bad = true;
+    else units += units_of(span[r]);
+  }
+  // (the units' thousands tell whether their sum fits 32 bits)
+  int total = __builtin_amdgcn_readlane(sum_upto(units), 63), thousands = __builtin_amdgcn_readlane(sum_upto((units + 1023) / 1024), 63);
+  if (__any(p.bad)) thousands = kMostUnits;
+  if (!alone) {
+    if (lane == 0) {
+      s_sums[0][wave] = total;
+      s_sums[1][wave] = min(thousands, kMostUnits / 1024 + 1);
+    }
+    if (threadIdx.x == 0) s_found = p;
+    __syncthreads();
+    total = thousands = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      total += s_sums[0][w];
+      thousands += s_sums[1][w];
+    }
+    total = uniform(total);
+    thousands = uniform(thousands);
+  }
+  p.bad = thousands > kMostUnits / 1024;
+  if (p.bad) return p;
+  // every stream's last piece is shorter: as many pieces as there are places, and one more a stream
+  const int room = max(a.places / 2, a.places - B);
+  const int length = max(least, (total + room - 1) / room);
+  p.length = length;
+  const float per_length = 1.0f / (float)length;
+  int pieces[R], upto[R], before = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (r >= rows) break;
+    // ceil(units / length): units are below 2^24, the product may be one off
+    const int n = units_of(span[r]);
+    int q = (int)((float)n * per_length);
+    q += q * length < n ? 1 : 0;
+    q += q * length < n ? 1 : 0;
+    pieces[r] = q - ((q - 1) * length >= n ? 1 : 0);
+    upto[r] = before + sum_upto(pieces[r]);
+    before = __builtin_amdgcn_readlane(upto[r], 63);
+  }
+  if (!alone) {
+    if (lane == 0) s_sums[2][wave] = before;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) piece -= s_sums[2][w];
+    piece = uniform(piece);
+  }
+  if (piece >= 0 && piece < before) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= rows) break;
+      const uint64_t in = __ballot(upto[r] > piece);
+      if (in == 0) continue;
+      const int l = __ffsll((unsigned long long)in) - 1;
+      p.stream = b0 + 64 * r + l;
+      p.pieces = __builtin_amdgcn_readlane(pieces[r], l);
+      p.number = piece - (__builtin_amdgcn_readlane(upto[r], l) - p.pieces);
+      p.first = __builtin_amdgcn_readlane(span[r].x, l);
+      p.held = __builtin_amdgcn_readlane(span[r].y, l);
+      break;
+    }
+    if (!alone && lane == 0) s_found = p;
+  }
+  if (!alone) {
+    __syncthreads();
+    p.stream = uniform(s_found.stream);
+    p.pieces = uniform(s_found.pieces);
+    p.number = uniform(s_found.number);
+    p.first = uniform(s_found.first);
+    p.held = uniform(s_found.held);
+  }
+  return p;
+}
+
+// n / d for small numbers (n < 2^16), without the long division.
+__device__ __forceinline__ int quotient(int n, float one_over_d) { return (int)(((float)n + 0.5f) * one_over_d); }
 
 // Workgroup: one piece of a stream and a.wave_slabs of the slabs; its NW wavefronts have one slab each, and where
 // that leaves some over, every second, third, .. tile of it.
 template <typename Core, int DH, int NW>
-__global__ __launch_bounds__(64 * NW, kPlaces * NW / 4) void memory_attention_kernel(MemoryAttentionArgs a) {
+__global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_kernel(MemoryAttentionArgs a) {
   typedef typename Core::T T;
   typedef typename Core::Result Result;
-  constexpr int kThreads = 64 * NW;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  __shared__ int s_wave[2][NW], s_flag;
-  int* const s_piece = reinterpret_cast<int*>(smem + kLds<Core, NW>);   // [B + 1] pieces of the streams before
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = uniform(tid >> 6);
-  const int B = a.B, G = a.heads / a.kv_heads;
-
-  // units of all streams
-  if (tid == 0) s_flag = 0;
-  __syncthreads();
-  const int per = (B + kThreads - 1) / kThreads, b0 = tid * per, b1 = min(B, b0 + per);
-  auto units_of = [](int2 span) { return span.y > 0 ? (span.x + span.y - 1) / kUnit - span.x / kUnit + 1 : 0; };
-  int mine = 0;
-  bool bad = false;
-  for (int b = b0; b < b1; ++b) {
-    const int2 span = a.span[b];
-    const bool wrong = span_is_bad(span.x, span.y, a.page_bits, a.cols);
-    bad |= wrong;
-    const int units = wrong ? 0 : units_of(span);
-    s_piece[b] = units;
-    mine += units;
-  }
-  if (bad) s_flag = 1;
-  // (a thread's units are below 2^28; their thousands tell whether the sum fits 32 bits)
-  const int upto_all = sum_upto(mine), thousands = sum_upto((mine + 1023) / 1024);
-  if (lane == 63) {
-    s_wave[0][wave] = upto_all;
-    s_wave[1][wave] = thousands;
-  }
-  __syncthreads();
-  int total = 0, all_thousands = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    total += s_wave[0][w];
-    all_thousands += s_wave[1][w];
-  }
-  total = uniform(total);
-  if (s_flag || all_thousands > kMostUnits / 1024) {
+  constexpr int kThreads = 64 * NW, Q = DH / 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[std::max(NW * Core::kBytes, kThreads * (int)sizeof(Sum))];
+  __shared__ int s_last;
+  const int tid = threadIdx.x, wave = uniform(tid >> 6);
+  const int G = a.heads / a.kv_heads;
+  const int passes = (G + Core::kGroup - 1) / Core::kGroup, slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
+  const int WS = a.wave_slabs, TS = NW / WS, slab_groups = slabs / WS;
+  const int number = blockIdx.x / slab_groups, slab_group = blockIdx.x - number * slab_groups;
+  const Piece p = find_piece<NW>(a, number, kLeast * TS);
+  if (p.bad) {
     if (blockIdx.x == 0 && tid == 0) *a.err_flag = 1;
     return;
   }
-  // the pieces' length, and how many there are of every stream: each stream's last one is shorter, so a piece a stream is left over
-  const int passes = (G + Core::kGroup - 1) / Core::kGroup, slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
-  const int WS = a.wave_slabs, TS = NW / WS, slab_groups = slabs / WS;
-  const int room = max(a.places / 2, a.places - B), length = max(kLeast * TS, (total + room - 1) / room);
-  mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int pieces = (s_piece[b] + length - 1) / length;
-    s_piece[b] = mine;
-    mine += pieces;
-  }
-  const int upto = sum_upto(mine);
-  __syncthreads();
-  if (lane == 63) s_wave[0][wave] = upto;
-  __syncthreads();
-  int base = upto - mine;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) base += w < wave ? s_wave[0][w] : 0;
-  for (int b = b0; b < b1; ++b) s_piece[b] += base;
-  if (tid == kThreads - 1) s_piece[B] = base + mine;
-  __syncthreads();
-
-  // rows of streams that hold nothing
-  for (int b = blockIdx.x; b < B; b += gridDim.x)
-    if (s_piece[b + 1] == s_piece[b])
-      for (int i = tid; i < a.heads * DH / 4; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)b * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
-
-  const int piece = blockIdx.x / slab_groups, slab_group = blockIdx.x - piece * slab_groups;
-  if (piece >= s_piece[B]) return;
-  const int b = uniform(stream_of(s_piece, B, piece));
-  const int piece0 = uniform(s_piece[b]), pieces = uniform(s_piece[b + 1]) - piece0;
-  const int first = uniform(a.span[b].x), held = uniform(a.span[b].y);
-  const int u0 = (piece - piece0) * length, u1 = min(u0 + length, units_of(make_int2(first, held)));
+  // the row of a stream that holds nothing (there are more workgroups than streams)
+  if ((int)blockIdx.x < a.B && a.span[blockIdx.x].y == 0)
+    for (int i = tid; i < a.heads * Q; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)blockIdx.x * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
+  if (p.stream < 0) return;
+  const int b = p.stream, u0 = p.number * p.length, u1 = min(u0 + p.length, units_of(make_int2(p.first, p.held)));
   const int my_slab = slab_group * WS + wave % WS;
-  Core::run(a, smem + wave * Core::kBytes, b, my_slab / passes, my_slab % passes, u0 + wave / WS, TS, u1, first, first + held);
+  Core::run(a, smem + wave * Core::kBytes, b, my_slab / passes, my_slab % passes, u0 + wave / WS, TS, u1, p.first, p.first + p.held);
   __syncthreads();
 
-  // the wavefronts' rows of a query head to one maximum, and added
-  for (int i = tid; i < WS * Core::kRows * (DH / 4); i += kThreads) {
-    const int quad = i % (DH / 4), row = i / (DH / 4) % Core::kRows, w = i / (DH / 4) / Core::kRows;
-    const int s = slab_group * WS + w, kh = s / passes * Core::kSlabHeads + row / Core::kGroup, in_group = s % passes * Core::kGroup + row % Core::kGroup;
-    if (kh >= a.kv_heads || in_group >= G) continue;
-    const int head = kh * G + in_group;
+  // The wavefronts' rows of a query head to one maximum, and added: a thread has four columns.  The group's query heads lie one
+  // behind the other: those of a slab's key heads, or a group of those of one key head.
+  const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
+  const int items = heads * Q;
+  const float per_key = 1.0f / (float)G;
+  for (int i = tid; i < items; i += kThreads) {
+    const int quad = i % Q, head = head0 + i / Q;
+    const int kh = quotient(head, per_key), in_key = head - kh * G;
+    const int slab = kh / Core::kSlabHeads * passes + in_key / Core::kGroup, row = kh % Core::kSlabHeads * Core::kGroup + in_key % Core::kGroup;
     Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    for (int p = 0; p < TS; ++p) {
-      const Result* const r = reinterpret_cast<const Result*>(smem + (p * WS + w) * Core::kBytes);
+    for (int part = 0; part < TS; ++part) {
+      const Result* const r = reinterpret_cast<const Result*>(smem + (part * WS + slab - slab_group * WS) * Core::kBytes);
       sum.add(Sum{r->m[row], r->l[row], *reinterpret_cast<const float4*>(&r->o[row][4 * quad])});
     }
-    if (pieces == 1) {
+    if (p.pieces == 1) {
       sum.store(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad);
     } else {
-      const size_t at = (size_t)piece * a.heads + head;
+      const size_t at = (size_t)number * a.heads + head;
       if (quad == 0) put2(a.partial_ml + at, make_float2(sum.m, sum.l));
       float2* const to = reinterpret_cast<float2*>(a.partial + at * DH + 4 * quad);
       put2(to, make_float2(sum.o.x, sum.o.y));
       put2(to + 1, make_float2(sum.o.z, sum.o.w));
     }
   }
-  if (pieces == 1) return;
+  if (p.pieces == 1) return;
   // the pieces of a stream: the workgroup that ends last adds them up, in order
   asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // (a piece has arrived in memory before its workgroup is counted)
   __syncthreads();
   if (tid == 0) {
     int32_t* const ticket = a.tickets + (size_t)b * slab_groups + slab_group;
-    s_flag = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
-    if (s_flag) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.pieces - 1;
+    if (s_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  if (!s_flag) return;
-  // the group's query heads, one behind the other; as many threads a quad of columns as there are
-  const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
-  const int items = heads * (DH / 4), parts = max(1, kThreads / items);
+  if (!s_last) return;
+  // as many threads four columns as there are
+  const int parts = max(1, kThreads / items);
   Sum* const s_sum = reinterpret_cast<Sum*>(smem);
   for (int i0 = 0; i0 < items; i0 += kThreads) {
-    const int item = i0 + (parts > 1 ? tid % items : tid), part = parts > 1 ? tid / items : 0;
-    const int head = head0 + item / (DH / 4), quad = item % (DH / 4);
+    const int part = parts > 1 ? quotient(tid, 1.0f / (float)items) : 0, item = i0 + tid - part * items;
+    const int head = head0 + item / Q, quad = item % Q;
     Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
     if (item < items && part < parts) {
       // (four at a time: loads of device scope are not moved past what is done with the one before)
       constexpr int N = 4;
-      for (int r = part; r < pieces; r += N * parts) {
+      for (int r = part; r < p.pieces; r += N * parts) {
         float2 ml[N], lo[N], hi[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-          const size_t at = (size_t)(piece0 + min(r + n * parts, pieces - 1)) * a.heads + head;
+          const size_t at = (size_t)(number - p.number + min(r + n * parts, p.pieces - 1)) * a.heads + head;
           const float2* const from = reinterpret_cast<const float2*>(a.partial + at * DH + 4 * quad);
           ml[n] = get2(a.partial_ml + at);
           lo[n] = get2(from);
@@ -567,14 +619,14 @@ __global__ __launch_bounds__(64 * NW, kPlaces * NW / 4) void memory_attention_ke
         }
 #pragma unroll
         for (int n = 0; n < N; ++n)
-          if (r + n * parts < pieces) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
+          if (r + n * parts < p.pieces) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
       }
     }
     if (parts > 1) {
       s_sum[tid] = sum;
       __syncthreads();
       if (part == 0)
-        for (int p = 1; p < parts; ++p) sum.add(s_sum[p * items + tid]);
+        for (int n = 1; n < parts; ++n) sum.add(s_sum[n * items + tid]);
     }
     if (item < items && part == 0) sum.store(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad);
   }
@@ -587,10 +639,7 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   a.wave_slabs = NW % 4 == 0 && slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
   a.places = std::max(1, kPlaces * cus / slab_groups);
-  const size_t lds = kLds<Core, NW> + (size_t)(a.B + 1) * sizeof(int);
-  static DeviceOnce once;
-  if (hipError_t e = allow_lds(memory_attention_kernel<Core, DH, NW>, kLds<Core, NW> + (kMemoryMaxStreams + 1) * sizeof(int), &once); e != hipSuccess) return e;
-  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), lds, s, a);
+  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), 0, s, a);
   return hipGetLastError();
 }
 
