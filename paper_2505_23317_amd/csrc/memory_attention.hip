@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kUnit = 32;             // tokens
 constexpr int kLeast = 4;             // units a wavefront that a piece has at least
+constexpr int kUncut = 10;            // and that a stream has at most to be one piece
 constexpr int kWaves = 8, kDepth = 1; // wavefronts of a workgroup, tiles that each has asked for
 constexpr int kPlaces = 2;            // workgroups a CU at once, for which streams are cut and pieces have room in memory
 constexpr int kMostUnits = 1 << 30;   // of all streams
@@ -494,7 +495,7 @@ __device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int pi
     int q = (int)((float)n * per_length);
     q += q * length < n ? 1 : 0;
     q += q * length < n ? 1 : 0;
-    pieces[r] = q - ((q - 1) * length >= n ? 1 : 0);
+    pieces[r] = n <= kUncut * (least / kLeast) ? min(n, 1) : q - ((q - 1) * length >= n ? 1 : 0);
     upto[r] = before + sum_upto(pieces[r]);
     before = __builtin_amdgcn_readlane(upto[r], 63);
   }
@@ -557,7 +558,8 @@ __global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_ke
   if ((int)blockIdx.x < a.B && a.span[blockIdx.x].y == 0)
     for (int i = tid; i < a.heads * Q; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)blockIdx.x * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
   if (p.stream < 0) return;
-  const int b = p.stream, u0 = p.number * p.length, u1 = min(u0 + p.length, units_of(make_int2(p.first, p.held)));
+  const int b = p.stream, units = units_of(make_int2(p.first, p.held));
+  const int u0 = p.number * p.length, u1 = p.pieces == 1 ? units : min(u0 + p.length, units);
   const int my_slab = slab_group * WS + wave % WS;
   Core::run(a, smem + wave * Core::kBytes, b, my_slab / passes, my_slab % passes, u0 + wave / WS, TS, u1, p.first, p.first + p.held);
   __syncthreads();
