@@ -819,24 +819,22 @@ class Encoder:
                        pool_out=None):
         """cu_new: int32 [B + 1]; span: int32 [B, 2]; table: int32 [B, max_pages]; pool: int32 [2]; free_pages: int32
         [n_pages]; slots: int32 [n_new] out; drop: int32 [B] or None.  The outputs are the inputs where they are not given."""
-        m, gpu = self._memory(), self.gpu
+        import torch
+        m, gpu, i32 = self._memory(), self.gpu, torch.int32
         B, n_new = span.shape[0], slots.shape[0]
-        _expect(cu_new, "int32", "cu_new", (B + 1,), gpu)
-        _expect(slots, "int32", "slots", (n_new,), gpu)
-        _expect(free_pages, "int32", "free_pages", (m.n_pages,), gpu)
-        if drop is not None:
-            _expect(drop, "int32", "drop", (B,), gpu)
-        both = []
-        for t, out, what, shape in ((span, span_out, "span", (B, 2)), (table, table_out, "table", (B, m.max_pages)),
-                                    (pool, pool_out, "pool", (2,))):
-            _expect(t, "int32", what, shape, gpu)
-            if out is None:
-                out = t
-            elif out is not t:
-                _expect(out, "int32", what + "_out", shape, gpu)
-            both += [t.data_ptr(), out.data_ptr()]
-        cfdetr_memory_advance(self.ctx, B, _ptr(drop), cu_new.data_ptr(), n_new, *both, free_pages.data_ptr(),
-                              slots.data_ptr(), self._stream())
+        wide, rows = (B, 2), (B, m.max_pages)
+        checks = [(cu_new, (B + 1,), "cu_new"), (slots, (n_new,), "slots"), (free_pages, (m.n_pages,), "free_pages"), (span, wide, "span"),
+                  (table, rows, "table"), (pool, (2,), "pool")]
+        for t, shape, what in ((drop, (B,), "drop"), (span_out, wide, "span_out"), (table_out, rows, "table_out"), (pool_out, (2,), "pool_out")):
+            if t is not None:
+                checks.append((t, shape, what))
+        for t, shape, what in checks:
+            # (what _expect asks for, without a call for each of ten tensors: 8.4 us a step with them)
+            if t.dtype is not i32 or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+                _expect(t, "int32", what, shape, gpu)
+        cfdetr_memory_advance(self.ctx, B, _ptr(drop), cu_new.data_ptr(), n_new, span.data_ptr(), (span if span_out is None else span_out).data_ptr(),
+                              table.data_ptr(), (table if table_out is None else table_out).data_ptr(), pool.data_ptr(),
+                              (pool if pool_out is None else pool_out).data_ptr(), free_pages.data_ptr(), slots.data_ptr(), self._stream())
 
     def rotary_axes(self, params: CfdetrRotaryAxesParams, freq, axis, pos, q, q_out, k=None, k_out=None, q_scale=1.0):
         """freq: float64, axis: uint8 [rot_dim / 2]; pos: float32 [M, n_axes]; q and q_out: [M, d], k and k_out: [M, key
