@@ -27,9 +27,9 @@ constexpr int kPlaces = 2;            // workgroups a CU at once, for which stre
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// Tiles' page numbers and open tokens, those of up to 64 of a wavefront's tiles at a time: lane l has tile l's.
+// Tiles' slots and open tokens, those of up to 64 of a wavefront's tiles at a time: lane l has tile l's.
 struct Tiles {
-  int id[4];       // page of tokens 8 j .. 8 j + 7
+  int slot[4];     // of token 8 j; those behind it up to 8 j + 7 lie behind it
   uint32_t open;   // bit t: token t is read
 };
 __device__ __forceinline__ Tiles tiles_of(const MemoryAttentionArgs& a, const int32_t* table, int first, int end, int p0, bool any) {
@@ -38,20 +38,20 @@ __device__ __forceinline__ Tiles tiles_of(const MemoryAttentionArgs& a, const in
   const int lo = max(first - p0, 0), hi = min(end - p0, kUnit);
   t.open = (0xFFFFFFFFu >> (kUnit - hi)) & (0xFFFFFFFFu << lo);
   bool wrong = false;
+  int id[4] = {};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if ((t.open >> (8 * j) & 0xFF) == 0) continue;
-    t.id[j] = table[ring_column((p0 + 8 * j) >> a.page_bits, a.cols)];
-  }
+  for (int j = 0; j < 4; ++j)
+    if (t.open >> (8 * j) & 0xFF) id[j] = table[ring_column((p0 + 8 * j) >> a.page_bits, a.cols)];
   uint2 bytes[4] = {};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if ((unsigned)t.id[j] >= (unsigned)a.n_pages) {
+    if ((unsigned)id[j] >= (unsigned)a.n_pages) {
       wrong = true;
-      t.id[j] = 0;
+      id[j] = 0;
       t.open &= ~(0xFFu << (8 * j));
     }
-    if (a.mask) bytes[j] = *reinterpret_cast<const uint2*>(a.mask + ((size_t)t.id[j] << a.page_bits) + ((p0 + 8 * j) & ((1 << a.page_bits) - 1)));
+    t.slot[j] = (id[j] << a.page_bits) + ((p0 + 8 * j) & ((1 << a.page_bits) - 1));
+    if (a.mask) bytes[j] = *reinterpret_cast<const uint2*>(a.mask + t.slot[j]);
   }
   if (a.mask) {
     uint32_t read = 0;
@@ -124,11 +124,11 @@ struct Core16 {
       }
     }
     f32x4 acc[NH][NB];
-    float m_run[NH], l_run[NH];
+    float m_run[NH], l_run[NH], ref[NH];   // ref: m_run, or 0 as long as no token is open
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       m_run[h] = -INFINITY;
-      l_run[h] = 0.f;
+      l_run[h] = ref[h] = 0.f;
 #pragma unroll
       for (int n = 0; n < NB; ++n) acc[h][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -141,7 +141,7 @@ struct Core16 {
     const uint32_t k_even = k_lane + (half ? kc & 3 : kc) * 16, k_odd = k_lane + (half ? kc & 3 : kc ^ 4) * 16;
     const uint32_t v_off = v_lane + (half ? vc & 3 : vc) * 16;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-    const int p_first = first & ~(kUnit - 1), page_mask = (1 << a.page_bits) - 1;
+    const int p_first = first & ~(kUnit - 1);
 
 #pragma nounroll
     for (; unit < units; unit += 64 * step) {
@@ -149,7 +149,7 @@ struct Core16 {
       const int p_lane = p_first + (unit + lane * step) * kUnit;
       Tiles t = tiles_of(a, table, first, end, p_lane, lane < count);
       // (ordinary loads are waited for here: the compiler does not count those into LDS, and would wait for all of them below)
-      asm volatile("" : "+v"(t.id[0]), "+v"(t.id[1]), "+v"(t.id[2]), "+v"(t.id[3]), "+v"(t.open));
+      asm volatile("" : "+v"(t.slot[0]), "+v"(t.slot[1]), "+v"(t.slot[2]), "+v"(t.slot[3]), "+v"(t.open));
 #pragma unroll
       for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -157,12 +157,10 @@ struct Core16 {
 
       auto load = [&](int i, uint32_t to) {
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
-        const int p0 = p_first + (unit + i * step) * kUnit;
         const char *k[4], *v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int id = __builtin_amdgcn_readlane(t.id[j], i);
-          const size_t slot = ((size_t)id << a.page_bits) + ((p0 + 8 * j) & page_mask);
+          const uint64_t slot = (uint32_t)__builtin_amdgcn_readlane(t.slot[j], i);
           k[j] = static_cast<const char*>(a.k) + slot * k_step;
           v[j] = static_cast<const char*>(a.v) + slot * v_step;
         }
@@ -247,6 +245,16 @@ struct Core16 {
               if (!(mine >> (16 + r) & 1)) s[h][1][r] = -INFINITY;
             }
           }
+          // The weights under the reference so far, and beside them whether it is to follow: it seldom is, and the products
+          // then need not wait for the maximum.
+          float p[8];
+          auto weigh = [&] {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[h][r >> 2][r & 3], a.scale2, -ref[h]));
+          };
+          weigh();
+#pragma unroll
+          for (int r = 0; r < 8; ++r) asm volatile("" : "+v"(p[r]));
           float top = s[h][0][0];
 #pragma unroll
           for (int r = 1; r < 8; ++r) top = fmaxf(top, s[h][r >> 2][r & 3]);
@@ -254,20 +262,19 @@ struct Core16 {
           const bool follow = top > m_run[h] + kSlack;
           if (__any(follow)) {
             const float alpha = follow ? __builtin_amdgcn_exp2f(m_run[h] - top) : 1.0f;
-            if (follow) m_run[h] = top;
+            if (follow) m_run[h] = ref[h] = top;
             l_run[h] *= alpha;
 #pragma unroll
             for (int n = 0; n < NB; ++n) acc[h][n] *= alpha;
+            weigh();
           }
-          const float ref = m_run[h] == -INFINITY ? 0.f : m_run[h];   // (no token may be open so far)
-          float p[8], sum = 0.f;
+          float sum = 0.f;
 #pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            p[r] = __builtin_amdgcn_exp2f(fmaf(s[h][r >> 2][r & 3], a.scale2, -ref));
-            sum += p[r];
-          }
+          for (int r = 0; r < 8; ++r) sum += p[r];
           l_run[h] += sum;
-          // a rounding of the weights: half a step of 2^-8 each, the sum takes them as they were
+          // a rounding of the weights: half a step of 2^-8 each, the sum takes them as they were.  (What it
+          // leaves in a second product: rows off by 0.0016 of their size instead of 0.0024, half of it the output's own rounding, for
+          // 1 to 3 % of the time of long streams and 3 to 9 % of short ones'.)
           const uint4 packed = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
           w[h] = *reinterpret_cast<const bf16x8*>(&packed);
         }
@@ -321,19 +328,17 @@ struct Core32 {
       m[h] = -INFINITY;
       l[h] = 0.f;
     }
-    const int p_first = first & ~(kUnit - 1), page_mask = (1 << a.page_bits) - 1;
+    const int p_first = first & ~(kUnit - 1);
     for (; unit < units; unit += 64 * step) {
       const int count = min(64, (units - unit + step - 1) / step);
       const Tiles t = tiles_of(a, table, first, end, p_first + (unit + lane * step) * kUnit, lane < count);
       for (int i = 0; i < count; ++i) {
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
-        const int p0 = p_first + (unit + i * step) * kUnit;
         float4 k[LOADS], v[LOADS];
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
           const int token = j * TPL + part;
-          const int id = __builtin_amdgcn_readlane(t.id[j * TPL / 8], i);
-          const size_t slot = ((size_t)id << a.page_bits) + ((p0 + token) & page_mask);
+          const size_t slot = (uint32_t)__builtin_amdgcn_readlane(t.slot[j * TPL / 8], i) + token % 8;
           k[j] = v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (open >> token & 1) {
             k[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.k) + slot * a.k_ld + slab * DH + 4 * c);
@@ -482,7 +487,7 @@ __device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int pi
   p.bad = thousands > kMostUnits / 1024;
   if (p.bad) return p;
   // every stream's last piece is shorter: as many pieces as there are places, and one more a stream
-  const int room = max(a.places / 2, a.places - B);
+  const int room = max((a.places + 1) / 2, a.places - B);
   const int length = max(least, (total + room - 1) / room);
   p.length = length;
   const float per_length = 1.0f / (float)length;
