@@ -401,13 +401,27 @@ __device__ __forceinline__ void store4(T* to, float4 x) {
 // Pieces pass between workgroups of any XCD, whose L2s do not see each other's: every one is written past them (stores of device
 // scope, waited for before the workgroup is counted) and read past them.  A release and an acquire around the counter would do the
 // same for all of an L2: one stream of 200,003 tokens, width 768, 116 us so, 267 with them.
-__device__ __forceinline__ void put2(float2* to, float2 v) {
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(to), (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get2(const float2* from) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
+struct Shared {
+  __amdgpu_buffer_rsrc_t at;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  static constexpr int kDevice = 16;   // sc1
+  __device__ explicit Shared(void* p) : at(__builtin_amdgcn_make_buffer_rsrc(p, 0, 0x7FFFFFFF, 0x00027000)) {}
+  __device__ __forceinline__ void put(int i, float2 v) const {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(v.x), __float_as_uint(v.y)}, at, i * 8, 0, kDevice);
+  }
+  __device__ __forceinline__ void put(int i, float4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)}, at, i * 16, 0, kDevice);
+  }
+  __device__ __forceinline__ float2 get2(int i) const {
+    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(at, i * 8, 0, kDevice);
+    return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
+  }
+  __device__ __forceinline__ float4 get4(int i) const {
+    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(at, i * 16, 0, kDevice);
+    return make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
+  }
+};
 // Four columns of a row under a maximum.
 struct Sum {
   float m, l;
@@ -574,6 +588,7 @@ __global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_ke
   const int head0 = first_head<Core>(slab_group * WS, passes, G), heads = min(first_head<Core>((slab_group + 1) * WS, passes, G), a.heads) - head0;
   const int items = heads * Q;
   const float per_key = 1.0f / (float)G;
+  const Shared all_ml(a.partial_ml), all_rows(a.partial);
   for (int i = tid; i < items; i += kThreads) {
     const int quad = i % Q, head = head0 + i / Q;
     const int kh = quotient(head, per_key), in_key = head - kh * G;
@@ -586,11 +601,9 @@ __global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_ke
     if (p.pieces == 1) {
       sum.store(static_cast<T*>(a.out) + (size_t)b * a.out_ld + head * DH + 4 * quad);
     } else {
-      const size_t at = (size_t)number * a.heads + head;
-      if (quad == 0) put2(a.partial_ml + at, make_float2(sum.m, sum.l));
-      float2* const to = reinterpret_cast<float2*>(a.partial + at * DH + 4 * quad);
-      put2(to, make_float2(sum.o.x, sum.o.y));
-      put2(to + 1, make_float2(sum.o.z, sum.o.w));
+      const int at = number * a.heads + head;
+      if (quad == 0) all_ml.put(at, make_float2(sum.m, sum.l));
+      all_rows.put(at * Q + quad, sum.o);
     }
   }
   if (p.pieces == 1) return;
@@ -612,22 +625,35 @@ __global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_ke
     const int head = head0 + item / Q, quad = item % Q;
     Sum sum{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
     if (item < items && part < parts) {
-      // (four at a time: loads of device scope are not moved past what is done with the one before)
-      constexpr int N = 4;
-      for (int r = part; r < p.pieces; r += N * parts) {
-        float2 ml[N], lo[N], hi[N];
+      auto add = [&](int r, auto count) {
+        constexpr int N = decltype(count)::value;
+        float2 ml[N];
+        float4 o[N];
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-          const size_t at = (size_t)(number - p.number + min(r + n * parts, p.pieces - 1)) * a.heads + head;
-          const float2* const from = reinterpret_cast<const float2*>(a.partial + at * DH + 4 * quad);
-          ml[n] = get2(a.partial_ml + at);
-          lo[n] = get2(from);
-          hi[n] = get2(from + 1);
+          const int at = (number - p.number + min(r + n * parts, p.pieces - 1)) * a.heads + head;
+          ml[n] = all_ml.get2(at);
+          o[n] = all_rows.get4(at * Q + quad);
         }
+        float top = sum.m;
 #pragma unroll
-        for (int n = 0; n < N; ++n)
-          if (r + n * parts < p.pieces) sum.add(Sum{ml[n].x, ml[n].y, make_float4(lo[n].x, lo[n].y, hi[n].x, hi[n].y)});
-      }
+        for (int n = 0; n < N; ++n) {
+          if (r + n * parts >= p.pieces) ml[n] = make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, ml[n].x);
+        }
+        const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(sum.m - ref);
+        sum = Sum{top, sum.l * keep, make_float4(sum.o.x * keep, sum.o.y * keep, sum.o.z * keep, sum.o.w * keep)};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const float f = __builtin_amdgcn_exp2f(ml[n].x - ref);
+          sum.l = fmaf(ml[n].y, f, sum.l);
+          sum.o = make_float4(fmaf(o[n].x, f, sum.o.x), fmaf(o[n].y, f, sum.o.y), fmaf(o[n].z, f, sum.o.z), fmaf(o[n].w, f, sum.o.w));
+        }
+      };
+      int r = part;
+      for (; r + 4 * parts < p.pieces; r += 8 * parts) add(r, std::integral_constant<int, 8>{});
+      if (r + parts < p.pieces) add(r, std::integral_constant<int, 4>{});
+      else if (r < p.pieces) add(r, std::integral_constant<int, 1>{});
     }
     if (parts > 1) {
       s_sum[tid] = sum;
