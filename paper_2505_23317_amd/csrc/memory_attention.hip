@@ -19,11 +19,17 @@ namespace cfdetr {
 
 namespace {
 
-constexpr int kUnit = 32;             // tokens
-constexpr int kLeast = 4;             // units a wavefront that a piece has at least
-constexpr int kUncut = 10;            // and that a stream has at most to be one piece
-constexpr int kWaves = 8, kDepth = 1; // wavefronts of a workgroup, tiles that each has asked for
-constexpr int kPlaces = 2;            // workgroups a CU at once, for which streams are cut and pieces have room in memory
+constexpr int kUnit = 32;   // tokens
+// Measured as replays of a captured call, us.
+// A piece has four units a wavefront at least, a stream of up to ten is not cut: the adding of pieces takes 2 us and more, a tile
+// 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 9.9 (six units at least 11.1, eight 12.0); of 300: 8.4 (in two pieces 10.0); 64 of
+// 100 to 2,000, 256 wide, 16.1 (uncut up to sixteen 21.6, but 100 of 900 then 20.4 instead of 23.1).
+constexpr int kLeast = 4, kUncut = 10;
+// Eight wavefronts a workgroup, each with one tile asked for while it works on the one before, two workgroups a CU: 24 streams of 8,000 to
+// 64,000 46.7, 300 of up to 900 21.8, 1,024 of up to 100 20.2, one of 1,600 9.9.  Eight with two tiles and one workgroup a CU: 48.5,
+// 24.3, 31.3, 10.4; sixteen: 48.6, 26.1, 33.7, 13.3; four with one tile and four workgroups (cut for as many): 66, 24, 18.5 and 9.2.
+constexpr int kWaves = 8, kDepth = 1;
+constexpr int kResident = 2;   // workgroups that a CU has room for
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -98,7 +104,7 @@ struct Rows {
 template <int DH, int DEPTH>
 struct Core16 {
   typedef bf16_t T;
-  static constexpr int kWavesSimd = kPlaces * kWaves / 4;
+  static constexpr int kWavesSimd = kResident * kWaves / 4;
   static constexpr int kSlabHeads = 64 / DH, kGroup = 16, kRows = kSlabHeads * kGroup;
   static constexpr int kTile = 2 * kUnit * 128;    // LDS of a tile: keys, values
   static constexpr int kBytes = DEPTH * kTile;
@@ -500,8 +506,9 @@ __device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int pi
   }
   p.bad = thousands > kMostUnits / 1024;
   if (p.bad) return p;
-  // every stream's last piece is shorter: as many pieces as there are places, and one more a stream
-  const int room = max((a.places + 1) / 2, a.places - B);
+  // Every stream's last piece is shorter: at most as many pieces as the length would make of one stream, and one more a stream.
+  // Few streams: no more pieces than places.
+  const int room = 2 * B <= a.places ? a.places - B : a.places;
   const int length = max(least, (total + room - 1) / room);
   p.length = length;
   const float per_length = 1.0f / (float)length;
@@ -671,7 +678,9 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
   a.wave_slabs = NW % 4 == 0 && slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
-  a.places = std::max(1, kPlaces * cus / slab_groups);
+  // One workgroup a CU has enough asked for to keep memory busy; the CU's second place is for what streams leave over.  24 streams of
+  // 8,000 to 64,000, a fifth masked: 47 us, 51 with pieces for both places; 64 of 2,000 tokens, 256 wide, 26.8 and 28.0.
+  a.places = std::max(1, cus / slab_groups);
   hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), 0, s, a);
   return hipGetLastError();
 }
@@ -680,7 +689,7 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
 
 MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
   // (as many pieces as places and streams, and slabs as query heads, at most)
-  const uint64_t pieces = (uint64_t)(kPlaces * cus + max_streams) * heads;
+  const uint64_t pieces = (uint64_t)(cus + max_streams) * heads;
   return {pieces * sizeof(float2), pieces * d_head * sizeof(float), (uint64_t)max_streams * heads * sizeof(int32_t)};
 }
 
