@@ -307,13 +307,24 @@ struct Core16 {
   }
 };
 
-// fp32, the check mode: a wavefront has one key head and up to four query heads.  LPR lanes hold a row's pieces of 16 bytes, so
+// Sum of v over LANES (8 or 16) consecutive lanes, delivered to all of them, inside the vector unit.
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v) {
+  auto from = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, false)); };
+  v += from(std::integral_constant<int, 0xB1>{});    // quad_perm [1, 0, 3, 2]
+  v += from(std::integral_constant<int, 0x4E>{});    // quad_perm [2, 3, 0, 1]
+  v += from(std::integral_constant<int, 0x141>{});   // row_half_mirror: the other quad of eight
+  if constexpr (LANES == 16) v += from(std::integral_constant<int, 0x140>{});   // row_mirror: the other eight
+  return v;
+}
+
+// fp32, the check mode: a wavefront has one key head and up to GROUP query heads.  LPR lanes hold a row's pieces of 16 bytes, so
 // a load takes 64 / LPR tokens; each group of lanes has a maximum, sum and row of its own until the end.
-template <int DH>
+template <int DH, int GROUP>
 struct Core32 {
   typedef float T;
   static constexpr int kWavesSimd = 2;
-  static constexpr int kSlabHeads = 1, kGroup = 4, kRows = kGroup;
+  static constexpr int kSlabHeads = 1, kGroup = GROUP, kRows = kGroup;
   typedef Rows<kRows, DH> Result;
   static constexpr int kBytes = (sizeof(Result) + 255) / 256 * 256;
 
@@ -357,8 +368,7 @@ struct Core32 {
 #pragma unroll
           for (int j = 0; j < LOADS; ++j) {
             s[j] = fmaf(q[h].x, k[j].x, fmaf(q[h].y, k[j].y, fmaf(q[h].z, k[j].z, q[h].w * k[j].w)));
-#pragma unroll
-            for (int o = 1; o < LPR; o <<= 1) s[j] += __shfl_xor(s[j], o);
+            s[j] = row_sum<LPR>(s[j]);
             if (!(open >> (j * TPL + part) & 1)) s[j] = -INFINITY;
             top = fmaxf(top, s[j]);
           }
@@ -685,6 +695,13 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int DH>
+hipError_t launch32(const MemoryAttentionArgs& a, int cus, hipStream_t s) {
+  const int G = a.heads / a.kv_heads;
+  if (G == 1) return launch<Core32<DH, 1>, DH, kWaves>(a, cus, s);
+  return G == 2 ? launch<Core32<DH, 2>, DH, kWaves>(a, cus, s) : launch<Core32<DH, 4>, DH, kWaves>(a, cus, s);
+}
+
 }  // namespace
 
 MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
@@ -694,8 +711,8 @@ MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_he
 }
 
 hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, int cus, hipStream_t s) {
-  if (d_head == 64) return use_bf16 ? launch<Core16<64, kDepth>, 64, kWaves>(a, cus, s) : launch<Core32<64>, 64, kWaves>(a, cus, s);
-  if (d_head == 32) return use_bf16 ? launch<Core16<32, kDepth>, 32, kWaves>(a, cus, s) : launch<Core32<32>, 32, kWaves>(a, cus, s);
+  if (d_head == 64) return use_bf16 ? launch<Core16<64, kDepth>, 64, kWaves>(a, cus, s) : launch32<64>(a, cus, s);
+  if (d_head == 32) return use_bf16 ? launch<Core16<32, kDepth>, 32, kWaves>(a, cus, s) : launch32<32>(a, cus, s);
   return hipErrorInvalidValue;
 }
 
