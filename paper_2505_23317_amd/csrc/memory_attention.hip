@@ -95,10 +95,10 @@ struct Rows {
   float o[ROWS][DH];
 };
 
-// bf16.  A wavefront has 128 bytes of every key and value row, a slab: NH key heads, and up to 16 query heads of each.
+// bf16, several query heads a key head.  A wavefront has 128 bytes of every key and value row, a slab: NH key heads, and up to 16 query heads of each.
 // Logits are products of 16 tokens x 32 features x 16 query heads, S^T = K Q^T, which leave lane l query head l mod 16 and tokens
 // 4 (l / 16) + r of either half of the tile; these are at once the operand of O^T = V^T P^T if the products' index runs over
-// the tokens in that order, so weights never leave their lane.  With one query head of 16 the products are 15 parts zeros and still cost a
+// the tokens in that order, so weights never leave their lane.  Two query heads of 16 leave the products 14 parts zeros, and still they cost a
 // fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own, DEPTH tiles ahead: no barrier in
 // the loop.
 template <int DH, int DEPTH>
@@ -279,7 +279,7 @@ struct Core16 {
           for (int r = 0; r < 8; ++r) sum += p[r];
           l_run[h] += sum;
           // a rounding of the weights: half a step of 2^-8 each, the sum takes them as they were.  (What it
-          // leaves in a second product: rows off by 0.0016 of their size instead of 0.0024, half of it the output's own rounding, for
+          // leaves in a second product: rows off by 0.0017 of their size instead of 0.0023, most of it the output's own rounding, for
           // 1 to 3 % of the time of long streams and 3 to 9 % of short ones'.)
           const uint4 packed = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
           w[h] = *reinterpret_cast<const bf16x8*>(&packed);
@@ -307,102 +307,179 @@ struct Core16 {
   }
 };
 
-// Sum of v over LANES (8 or 16) consecutive lanes, delivered to all of them, inside the vector unit.
+// Sum of v over LANES (4, 8 or 16) consecutive lanes, delivered to all of them, inside the vector unit.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v) {
   auto from = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF, 0xF, false)); };
   v += from(std::integral_constant<int, 0xB1>{});    // quad_perm [1, 0, 3, 2]
   v += from(std::integral_constant<int, 0x4E>{});    // quad_perm [2, 3, 0, 1]
-  v += from(std::integral_constant<int, 0x141>{});   // row_half_mirror: the other quad of eight
+  if constexpr (LANES >= 8) v += from(std::integral_constant<int, 0x141>{});    // row_half_mirror: the other quad of eight
   if constexpr (LANES == 16) v += from(std::integral_constant<int, 0x140>{});   // row_mirror: the other eight
   return v;
 }
 
-// fp32, the check mode: a wavefront has one key head and up to GROUP query heads.  LPR lanes hold a row's pieces of 16 bytes, so
-// a load takes 64 / LPR tokens; each group of lanes has a maximum, sum and row of its own until the end.
-template <int DH, int GROUP>
-struct Core32 {
-  typedef float T;
+// 16 bytes of a row.
+template <typename T>
+struct Bytes16;
+template <>
+struct Bytes16<bf16_t> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ float dot(const uint4& a, const uint4& b) {
+    auto two = [](uint32_t x, uint32_t y, float c) {
+      return __builtin_amdgcn_fdot2_f32_bf16(*reinterpret_cast<const bf16x2*>(&x), *reinterpret_cast<const bf16x2*>(&y), c, false);
+    };
+    return two(a.x, b.x, two(a.y, b.y, two(a.z, b.z, two(a.w, b.w, 0.f))));
+  }
+  static __device__ __forceinline__ void get(const uint4& v, float (&x)[kN]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+};
+template <>
+struct Bytes16<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ float dot(const uint4& a, const uint4& b) {
+    auto f = [](uint32_t x) { return __uint_as_float(x); };
+    return fmaf(f(a.x), f(b.x), fmaf(f(a.y), f(b.y), fmaf(f(a.z), f(b.z), f(a.w) * f(b.w))));
+  }
+  static __device__ __forceinline__ void get(const uint4& v, float (&x)[kN]) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+  }
+};
+
+// One query head a key head, and fp32 (the check mode): a wavefront has 128 bytes or a head of every row, and up to GROUP query heads of a
+// key head.  Lanes hold a row's pieces of 16 bytes, LANES of them a token, so a load takes 64 / LANES tokens; each group of lanes has
+// a maximum, sum and row of its own until the end.  Weights stay in 32 bits.
+template <typename E, int DH, int GROUP>
+struct CoreLanes {
+  typedef E T;
+  static constexpr int N = Bytes16<E>::kN, kPieces = DH / N;   // of a head
   static constexpr int kWavesSimd = 2;
-  static constexpr int kSlabHeads = 1, kGroup = GROUP, kRows = kGroup;
+  static constexpr int kSlabHeads = kPieces < 8 ? 8 / kPieces : 1, kGroup = GROUP, kRows = kSlabHeads * GROUP;
   typedef Rows<kRows, DH> Result;
   static constexpr int kBytes = (sizeof(Result) + 255) / 256 * 256;
 
   static __device__ __forceinline__ void run(const MemoryAttentionArgs& a, unsigned char* lds, int b, int slab, int group, int unit, int step,
                                              int units, int first, int end) {
-    constexpr int LPR = DH / 4, TPL = 64 / LPR, LOADS = kUnit / TPL;
-    const int lane = threadIdx.x & 63, part = lane / LPR, c = lane % LPR;
+    constexpr int LANES = kSlabHeads * kPieces, TPL = 64 / LANES, LOADS = kUnit / TPL;
+    static_assert(LANES >= 8, "the tokens of a load lie behind each other");
+    const int lane = threadIdx.x & 63, part = lane / LANES, in_slab = lane % LANES / kPieces, c = lane % kPieces;
     const int G = a.heads / a.kv_heads;
+    const int kh = min(slab * kSlabHeads + in_slab, a.kv_heads - 1);   // (a slab's last head again, where there are fewer)
     const int32_t* const table = a.table + (size_t)b * a.cols;
-    float4 q[kGroup], acc[kGroup];
-    float m[kGroup], l[kGroup];
+    uint4 q[GROUP];
+    float acc[GROUP][N], m[GROUP], l[GROUP];
 #pragma unroll
-    for (int h = 0; h < kGroup; ++h) {
-      const int head = slab * G + min(group * kGroup + h, G - 1);   // (a group's last head again, where there are fewer)
-      const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (size_t)b * a.q_ld + head * DH + 4 * c);
-      q[h] = make_float4(v.x * a.scale2, v.y * a.scale2, v.z * a.scale2, v.w * a.scale2);
-      acc[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int h = 0; h < GROUP; ++h) {
+      const int head = kh * G + min(group * GROUP + h, G - 1);   // (and a group's)
+      q[h] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + (size_t)b * a.q_ld + head * DH + N * c);
       m[h] = -INFINITY;
       l[h] = 0.f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[h][e] = 0.f;
     }
     const int p_first = first & ~(kUnit - 1);
+    const uint32_t column = (kh * DH + N * c) * (uint32_t)sizeof(T);
+    const uint32_t k_step = (uint32_t)a.k_ld * (uint32_t)sizeof(T), v_step = (uint32_t)a.v_ld * (uint32_t)sizeof(T);
+    const uint32_t k_lane = part * k_step + column, v_lane = part * v_step + column;
     for (; unit < units; unit += 64 * step) {
       const int count = min(64, (units - unit + step - 1) / step);
       const Tiles t = tiles_of(a, table, first, end, p_first + (unit + lane * step) * kUnit, lane < count);
       for (int i = 0; i < count; ++i) {
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
-        float4 k[LOADS], v[LOADS];
+        uint4 k[LOADS], v[LOADS];
+        const char *k_from[LOADS], *v_from[LOADS];
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-          const int token = j * TPL + part;
-          const size_t slot = (uint32_t)__builtin_amdgcn_readlane(t.slot[j * TPL / 8], i) + token % 8;
-          k[j] = v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (open >> token & 1) {
-            k[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.k) + slot * a.k_ld + slab * DH + 4 * c);
-            v[j] = *reinterpret_cast<const float4*>(static_cast<const float*>(a.v) + slot * a.v_ld + slab * DH + 4 * c);
-          }
+          const uint64_t slot = (uint32_t)__builtin_amdgcn_readlane(t.slot[j * TPL / 8], i) + j * TPL % 8;
+          k_from[j] = static_cast<const char*>(a.k) + slot * k_step;
+          v_from[j] = static_cast<const char*>(a.v) + slot * v_step;
+        }
+        if (open == 0xFFFFFFFFu) {
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) k[j] = *reinterpret_cast<const uint4*>(k_from[j] + k_lane);
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) v[j] = *reinterpret_cast<const uint4*>(v_from[j] + v_lane);
+        } else {
+          // tokens that are not read: zeros, from the one place that all such lanes share
+          const char* const zeros = static_cast<const char*>(a.zeros);
+          const uint32_t mine = open >> part;
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) k[j] = *reinterpret_cast<const uint4*>(mine >> (j * TPL) & 1 ? k_from[j] + k_lane : zeros);
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) v[j] = *reinterpret_cast<const uint4*>(mine >> (j * TPL) & 1 ? v_from[j] + v_lane : zeros);
+        }
+        float s[GROUP][LOADS];
+#pragma unroll
+        for (int h = 0; h < GROUP; ++h)
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) s[h][j] = row_sum<kPieces>(Bytes16<T>::dot(q[h], k[j])) * a.scale2;
+        if (open != 0xFFFFFFFFu) {
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j)
+            if (!(open >> (j * TPL + part) & 1))
+#pragma unroll
+              for (int h = 0; h < GROUP; ++h) s[h][j] = -INFINITY;
         }
 #pragma unroll
-        for (int h = 0; h < kGroup; ++h) {
-          float s[LOADS], top = m[h];
+        for (int h = 0; h < GROUP; ++h) {
+          float top = m[h];
 #pragma unroll
-          for (int j = 0; j < LOADS; ++j) {
-            s[j] = fmaf(q[h].x, k[j].x, fmaf(q[h].y, k[j].y, fmaf(q[h].z, k[j].z, q[h].w * k[j].w)));
-            s[j] = row_sum<LPR>(s[j]);
-            if (!(open >> (j * TPL + part) & 1)) s[j] = -INFINITY;
-            top = fmaxf(top, s[j]);
-          }
+          for (int j = 0; j < LOADS; ++j) top = fmaxf(top, s[h][j]);
           const float ref = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(m[h] - ref);
           m[h] = top;
           l[h] *= keep;
-          acc[h] = make_float4(acc[h].x * keep, acc[h].y * keep, acc[h].z * keep, acc[h].w * keep);
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[h][e] *= keep;
 #pragma unroll
           for (int j = 0; j < LOADS; ++j) {
-            const float w = __builtin_amdgcn_exp2f(s[j] - ref);
-            l[h] += w;
-            acc[h] = make_float4(fmaf(w, v[j].x, acc[h].x), fmaf(w, v[j].y, acc[h].y), fmaf(w, v[j].z, acc[h].z), fmaf(w, v[j].w, acc[h].w));
+            s[h][j] = __builtin_amdgcn_exp2f(s[h][j] - ref);
+            l[h] += s[h][j];
           }
+        }
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          float x[N];
+          Bytes16<T>::get(v[j], x);
+#pragma unroll
+          for (int h = 0; h < GROUP; ++h)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[h][e] = fmaf(s[h][j], x[e], acc[h][e]);
         }
       }
     }
     Result* const to = reinterpret_cast<Result*>(lds);
 #pragma unroll
-    for (int h = 0; h < kGroup; ++h) {
+    for (int h = 0; h < GROUP; ++h) {
       float top = m[h];
 #pragma unroll
-      for (int o = LPR; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      for (int o = LANES; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
       const float f = __builtin_amdgcn_exp2f(m[h] - (top == -INFINITY ? 0.f : top));
-      float sums[5] = {l[h] * f, acc[h].x * f, acc[h].y * f, acc[h].z * f, acc[h].w * f};
+      l[h] *= f;
 #pragma unroll
-      for (int o = LPR; o < 64; o <<= 1)
+      for (int e = 0; e < N; ++e) acc[h][e] *= f;
 #pragma unroll
-        for (int i = 0; i < 5; ++i) sums[i] += __shfl_xor(sums[i], o);
+      for (int o = LANES; o < 64; o <<= 1) {
+        l[h] += __shfl_xor(l[h], o);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[h][e] += __shfl_xor(acc[h][e], o);
+      }
       if (part == 0) {
+        const int row = in_slab * GROUP + h;
         if (c == 0) {
-          to->m[h] = top;
-          to->l[h] = sums[0];
+          to->m[row] = top;
+          to->l[row] = l[h];
         }
-        *reinterpret_cast<float4*>(&to->o[h][4 * c]) = make_float4(sums[1], sums[2], sums[3], sums[4]);
+#pragma unroll
+        for (int e = 0; e < N; e += 4)
+          *reinterpret_cast<float4*>(&to->o[row][N * c + e]) = make_float4(acc[h][e], acc[h][e + 1], acc[h][e + 2], acc[h][e + 3]);
       }
     }
   }
@@ -695,11 +772,20 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Key heads of one query head go through lanes, those of several through matrix products, whose time is that of 16.  bf16, us:
+// one query head, 256 wide in heads of 32: one stream of 1,600 tokens 10.2 by lanes, 11.0 by products; 1,024 of up to 100 18.4 and
+// 20.3; heads of 64, width 768: 10.5 and 9.9, one stream of 200,003 115.6 and 115.8, and rows off by 0.0017 of their size instead of
+// 0.0023 (lanes keep the weights in 32 bits).  Two query heads: one stream of 1,600, 256 / 4 key heads, 12.3 and 10.8, 300 of
+// up to 900 18.5 and 15.4.
 template <int DH>
-hipError_t launch32(const MemoryAttentionArgs& a, int cus, hipStream_t s) {
+hipError_t launch(const MemoryAttentionArgs& a, bool use_bf16, int cus, hipStream_t s) {
   const int G = a.heads / a.kv_heads;
-  if (G == 1) return launch<Core32<DH, 1>, DH, kWaves>(a, cus, s);
-  return G == 2 ? launch<Core32<DH, 2>, DH, kWaves>(a, cus, s) : launch<Core32<DH, 4>, DH, kWaves>(a, cus, s);
+  if (use_bf16) {
+    if (G == 1) return launch<CoreLanes<bf16_t, DH, 1>, DH, kWaves>(a, cus, s);
+    return launch<Core16<DH, kDepth>, DH, kWaves>(a, cus, s);
+  }
+  if (G == 1) return launch<CoreLanes<float, DH, 1>, DH, kWaves>(a, cus, s);
+  return G == 2 ? launch<CoreLanes<float, DH, 2>, DH, kWaves>(a, cus, s) : launch<CoreLanes<float, DH, 4>, DH, kWaves>(a, cus, s);
 }
 
 }  // namespace
@@ -711,8 +797,8 @@ MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_he
 }
 
 hipError_t launch_memory_attention(const MemoryAttentionArgs& a, int d_head, bool use_bf16, int cus, hipStream_t s) {
-  if (d_head == 64) return use_bf16 ? launch<Core16<64, kDepth>, 64, kWaves>(a, cus, s) : launch32<64>(a, cus, s);
-  if (d_head == 32) return use_bf16 ? launch<Core16<32, kDepth>, 32, kWaves>(a, cus, s) : launch32<32>(a, cus, s);
+  if (d_head == 64) return launch<64>(a, use_bf16, cus, s);
+  if (d_head == 32) return launch<32>(a, use_bf16, cus, s);
   return hipErrorInvalidValue;
 }
 

@@ -100,16 +100,17 @@ def attention(q, k_cache, v_cache, slots, heads, kv_heads, dtype, scale=None, ma
     Bound.  A logit's products (d_head of them, the scale) are rounded in 32 bits: off by (d_head + 4) 2^-24 times
     scale sum |q k|, the largest of a row's logits making e.  The probability of a token is then off by 2 e, and 4 * 2^-24 more for
     the exponentials; n of them are added in 32 bits, under weights and alone (n 2^-24 twice).  So a row is off by
-    (4 e + (8 + 2 n) 2^-24) sum p |v|, and by half a step of its type once it is rounded.  In bf16 the weights are operands
-    of a matrix product and so rounded to bf16, the sum that divides is of the weights as they were: a weight w_t becomes
-    w_t (1 + r_t), |r_t| <= 2^-8, and the row sum w_t (1 + r_t) v_t / sum w_t is off by sum p_t |r_t v_t| <= 2^-8 sum p |v|, `u`.
+    (4 e + (8 + 2 n) 2^-24) sum p |v|, and by half a step of its type once it is rounded.  Where query heads share a key head,
+    bf16 weights are operands of a matrix product and so rounded to bf16, the sum that divides is of the weights as they were:
+    a weight w_t becomes w_t (1 + r_t), |r_t| <= 2^-8, and the row sum w_t (1 + r_t) v_t / sum w_t is off by
+    sum p_t |r_t v_t| <= 2^-8 sum p |v|, `u`.
     """
     import torch
     d = q.shape[1]
     dh = d // heads
     group = heads // kv_heads
     scale = dh ** -0.5 if scale is None else scale
-    u = T.HALF_STEP["bf16"] if dtype == "bf16" else 0.0
+    u = T.HALF_STEP["bf16"] if dtype == "bf16" and group > 1 else 0.0
     out = torch.zeros(q.shape[0], d, dtype=torch.float64, device="cuda")
     bound = torch.zeros_like(out)
     for b, at in enumerate(slots):
