@@ -20,15 +20,14 @@ namespace cfdetr {
 namespace {
 
 constexpr int kUnit = 32;   // tokens
-// Measured as replays of a captured call, us.
-// A piece has four units a wavefront at least, a stream of up to ten is not cut: the adding of pieces takes 2 us and more, a tile
-// 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 9.9 (six units at least 11.1, eight 12.0); of 300: 8.4 (in two pieces 10.0); 64 of
-// 100 to 2,000, 256 wide, 16.1 (uncut up to sixteen 21.6, but 100 of 900 then 20.4 instead of 23.1).
+// Measured as replays of a captured call, us; "768 / 4": width 768, four key heads.
+// A piece has four units a wavefront at least, a stream of up to ten is not cut: adding the pieces takes 2 us and more, a tile
+// 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 10.5 (six units at least 12.1, eight 13.6; six streams of 4,000 to 16,000, 768 / 4,
+// then 16.8 and 15.9 instead of 17.5); of 300: 9.1 (cut in two 10.2); 300 of up to 900, 256 wide, 21.4 (uncut up to sixteen 22.9, none 23.4).
 constexpr int kLeast = 4, kUncut = 10;
-// Eight wavefronts a workgroup, each with one tile asked for while it works on the one before, two workgroups a CU: 24 streams of 8,000 to
-// 64,000 46.7, 300 of up to 900 21.8, 1,024 of up to 100 20.2, one of 1,600 9.9.  Eight with two tiles and one workgroup a CU: 48.5,
-// 24.3, 31.3, 10.4; sixteen: 48.6, 26.1, 33.7, 13.3; four with one tile and four workgroups (cut for as many): 66, 24, 18.5 and 9.2.
-constexpr int kWaves = 8, kDepth = 1;
+// Eight wavefronts a workgroup, two workgroups a CU: 24 streams of 8,000 to 64,000, 768 / 2, 47.6, 300 of up to 900, 256 wide, 21.4, 1,024 of
+// up to 100 18.4, one of 1,600, width 768, 10.5.  Sixteen and one: 48.4, 24.4, 31.3, 13.6; four and four: 50.7, 23.5, 19.1, 9.8.
+constexpr int kWaves = 8;
 constexpr int kResident = 2;   // workgroups that a CU has room for
 constexpr int kMostUnits = 1 << 30;   // of all streams
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -99,15 +98,15 @@ struct Rows {
 // Logits are products of 16 tokens x 32 features x 16 query heads, S^T = K Q^T, which leave lane l query head l mod 16 and tokens
 // 4 (l / 16) + r of either half of the tile; these are at once the operand of O^T = V^T P^T if the products' index runs over
 // the tokens in that order, so weights never leave their lane.  Two query heads of 16 leave the products 14 parts zeros, and still they cost a
-// fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own, DEPTH tiles ahead: no barrier in
-// the loop.
-template <int DH, int DEPTH>
+// fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own, a tile ahead: no barrier in
+// the loop.  (Two tiles ahead leave a CU one workgroup: 24 streams of 8,000 to 64,000, 768 / 2, 50.0 instead of 47.6 us, 1,024 of up
+// to 100, 768 / 4, 30.3 instead of 19.1.)
+template <int DH>
 struct Core16 {
   typedef bf16_t T;
   static constexpr int kWavesSimd = kResident * kWaves / 4;
   static constexpr int kSlabHeads = 64 / DH, kGroup = 16, kRows = kSlabHeads * kGroup;
-  static constexpr int kTile = 2 * kUnit * 128;    // LDS of a tile: keys, values
-  static constexpr int kBytes = DEPTH * kTile;
+  static constexpr int kBytes = 2 * kUnit * 128;   // LDS of a tile: keys, values
   typedef Rows<kRows, DH> Result;
   static_assert(sizeof(Result) <= kBytes, "in place of keys and values");
 
@@ -146,6 +145,8 @@ struct Core16 {
     const uint32_t k_lane = (uint32_t)(lane >> 3) * k_step + slab * 128, v_lane = (uint32_t)(lane >> 3) * v_step + slab * 128;
     const uint32_t k_even = k_lane + (half ? kc & 3 : kc) * 16, k_odd = k_lane + (half ? kc & 3 : kc ^ 4) * 16;
     const uint32_t v_off = v_lane + (half ? vc & 3 : vc) * 16;
+    const unsigned char* const sK = lds;
+    const unsigned char* const sV = lds + kUnit * 128;
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int p_first = first & ~(kUnit - 1);
 
@@ -161,7 +162,7 @@ struct Core16 {
 #pragma unroll
         for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[h][s].x), "+v"(qf[h][s].y), "+v"(qf[h][s].z), "+v"(qf[h][s].w));
 
-      auto load = [&](int i, uint32_t to) {
+      auto load = [&](int i) {
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
         const char *k[4], *v[4];
 #pragma unroll
@@ -172,32 +173,23 @@ struct Core16 {
         }
         if (open == 0xFFFFFFFFu) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dma16(k[j], j & 1 ? k_odd : k_even, to + j * 1024);
+          for (int j = 0; j < 4; ++j) dma16(k[j], j & 1 ? k_odd : k_even, lds0 + j * 1024);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dma16(v[j], v_off, to + (4 + j) * 1024);
+          for (int j = 0; j < 4; ++j) dma16(v[j], v_off, lds0 + (4 + j) * 1024);
         } else {
           // tokens that are not read: zeros, from the one place that all such lanes share
           const char* const zeros = static_cast<const char*>(a.zeros);
           const uint32_t mine = open >> (lane >> 3);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? k[j] + (j & 1 ? k_odd : k_even) : zeros, to + j * 1024);
+          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? k[j] + (j & 1 ? k_odd : k_even) : zeros, lds0 + j * 1024);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? v[j] + v_off : zeros, to + (4 + j) * 1024);
+          for (int j = 0; j < 4; ++j) dma16(mine >> (8 * j) & 1 ? v[j] + v_off : zeros, lds0 + (4 + j) * 1024);
         }
       };
-      for (int i = 0; i < min(DEPTH, count); ++i) load(i, lds0 + i * kTile);
-      int place = 0;
+      load(0);
 #pragma nounroll
       for (int i = 0; i < count; ++i) {
-        // this tile's eight loads; those of the tiles behind it need not be there yet
-        const int behind = min(DEPTH, count - i) - 1;
-        if (behind == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-        else if (behind == 1) asm volatile("s_waitcnt vmcnt(8)" : : : "memory");
-        else if (behind == 2) asm volatile("s_waitcnt vmcnt(16)" : : : "memory");
-        else asm volatile("s_waitcnt vmcnt(24)" : : : "memory");
-        static_assert(DEPTH <= 4, "the counts above");
-        const unsigned char* const sK = lds + place;
-        const unsigned char* const sV = sK + kUnit * 128;
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         // all operands at once: the tile's place is free for the next loads before a product is taken, and no product waits for a read
         typedef __attribute__((ext_vector_type(4))) short s16x4;
         typedef __attribute__((address_space(3))) s16x4* lds4;
@@ -227,8 +219,7 @@ struct Core16 {
                   sV + row * 128 + ((h * NB + n) ^ ((row >> 1) & 3)) * 32 + (lane & 3) * 8));
             }
         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-        if (i + DEPTH < count) load(i + DEPTH, lds0 + place);
-        place = place + kTile == kBytes ? 0 : place + kTile;
+        if (i + 1 < count) load(i + 1);
         f32x4 s[NH][2];
 #pragma unroll
         for (int h = 0; h < NH; ++h)
@@ -766,7 +757,7 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   a.wave_slabs = NW % 4 == 0 && slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
   // One workgroup a CU has enough asked for to keep memory busy; the CU's second place is for what streams leave over.  24 streams of
-  // 8,000 to 64,000, a fifth masked: 47 us, 51 with pieces for both places; 64 of 2,000 tokens, 256 wide, 26.8 and 28.0.
+  // 8,000 to 64,000, a fifth masked: 47.6 us, 51.0 with pieces for both places; one of 200,003, width 768, 115.9 and 119.4.
   a.places = std::max(1, cus / slab_groups);
   hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), 0, s, a);
   return hipGetLastError();
@@ -782,7 +773,7 @@ hipError_t launch(const MemoryAttentionArgs& a, bool use_bf16, int cus, hipStrea
   const int G = a.heads / a.kv_heads;
   if (use_bf16) {
     if (G == 1) return launch<CoreLanes<bf16_t, DH, 1>, DH, kWaves>(a, cus, s);
-    return launch<Core16<DH, kDepth>, DH, kWaves>(a, cus, s);
+    return launch<Core16<DH>, DH, kWaves>(a, cus, s);
   }
   if (G == 1) return launch<CoreLanes<float, DH, 1>, DH, kWaves>(a, cus, s);
   return G == 2 ? launch<CoreLanes<float, DH, 2>, DH, kWaves>(a, cus, s) : launch<CoreLanes<float, DH, 4>, DH, kWaves>(a, cus, s);
