@@ -754,7 +754,7 @@ template <typename Core, int DH, int NW>
 hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   const int G = a.heads / a.kv_heads, passes = (G + Core::kGroup - 1) / Core::kGroup;
   const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
-  a.wave_slabs = NW % 4 == 0 && slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
+  a.wave_slabs = slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
   // One workgroup a CU has enough asked for to keep memory busy; the CU's second place is for what streams leave over.  24 streams of
   // 8,000 to 64,000, a fifth masked: 47.6 us, 51.0 with pieces for both places; one of 200,003, width 768, 115.9 and 119.4.

@@ -254,7 +254,7 @@ def test_refusals(K):
     for bad, status in ((dict(B=0), K.CFDETR_EINVAL), (dict(B=-1), K.CFDETR_EINVAL), (dict(B=3), K.CFDETR_ECAPACITY), (dict(scale=-1.0), K.CFDETR_EINVAL),
                         (dict(scale=math.nan), K.CFDETR_EINVAL), (dict(scale=math.inf), K.CFDETR_EINVAL),
                         *((dict([(name, value)]), K.CFDETR_EINVAL) for name in ("q", "k", "v", "out", "span", "table") for value in (None, p + 2)),
-                        (dict(span=n + 4), K.CFDETR_EINVAL), (dict(q_ld=56), K.CFDETR_EINVAL), (dict(k_ld=24), K.CFDETR_EINVAL), (dict(v_ld=36), K.CFDETR_EINVAL),
+                        (dict(span=n + 4), K.CFDETR_EINVAL), (dict(mask=n + 4), K.CFDETR_EINVAL), (dict(q_ld=56), K.CFDETR_EINVAL), (dict(k_ld=24), K.CFDETR_EINVAL), (dict(v_ld=36), K.CFDETR_EINVAL),
                         (dict(out_ld=88), K.CFDETR_EINVAL), (dict(k_ld=(1 << 24) + 8), K.CFDETR_EINVAL)):
         with pytest.raises(K.CfdetrError) as e:
             call(**bad)
