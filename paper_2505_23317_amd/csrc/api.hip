@@ -1506,7 +1506,7 @@ CFDETR_API cfdetr_status cfdetr_sync_status(cfdetr_ctx* ctx, void* hip_stream) {
   if (flag) {
     e = hipMemset(ctx->err_flag, 0, 4);
     if (e != hipSuccess) return fail_hip(ctx, "hipMemset", e);
-    return fail(ctx, CFDETR_ECAPACITY, "a device-side check failed: more tokens or regions than the context holds, or bad sequence offsets");
+    return fail(ctx, CFDETR_ECAPACITY, "a device-side check failed: more tokens or regions than the context holds, bad sequence offsets, or a memory's step or state that cannot be");
   }
   return CFDETR_OK;
 }

@@ -82,10 +82,11 @@ def test_head_layouts(K, d, kv, dtype, page):
 
 
 @pytest.mark.parametrize("heads,d", [(32, 1024), (10, 320), (5, 320), (14, 448), (7, 448), (9, 576), (3, 192), (20, 640), (1, 64)])
-def test_numbers_of_heads(K, heads, d):
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_numbers_of_heads(K, heads, d, dtype):
     """Every divisor of the heads as their number of key heads, odd groups among them."""
     for kv in (n for n in range(1, heads + 1) if heads % n == 0):
-        case = Case(d, kv, [130, 1, 77], 16, "bf16", seed=kv, heads=heads)
+        case = Case(d, kv, [130, 1, 77], 16, dtype, seed=kv, heads=heads)
         case.check(case.run())
         case.enc.close()
 
@@ -177,6 +178,63 @@ def test_scale(K):
     case.run(wide[:, 256:512], wide[:, 256:512])
     assert torch.equal(wide[:, 256:512], want) and not wide[:, :256].any() and not wide[:, 512:].any()
     case.enc.close()
+
+
+def test_streams_on_the_same_pages(K):
+    """A copied state: several streams read the same slots, fewer streams than the context may have."""
+    import torch
+    case = Case(256, 2, [900, 40, 3, 7, 1], 16, "bf16")
+    case.span[1:3], case.table[1:3] = case.span[0].clone(), case.table[0].clone()
+    case.span[2, 1] = 500   # (the first of them)
+    case.q[1] = case.q[0]
+    case.slots[1:3] = case.slots[0], case.slots[0][:500]
+    out = torch.empty(4, 256, device="cuda", dtype=torch.bfloat16)
+    case.enc.memory_attention(case.q[:4], case.k, case.v, case.span[:4], case.table[:4], out)
+    want, bound = R.attention(case.q[:4], case.k, case.v, case.slots[:4], 8, 2, "bf16")
+    T.within(out, want, bound)
+    assert torch.equal(out[0], out[1])
+    case.enc.sync_status()
+    case.enc.close()
+
+
+@pytest.mark.parametrize("d,kv,dtype", [(256, 8, "bf16"), (768, 2, "bf16"), (384, 6, "f32")])
+def test_values_that_are_no_numbers_stay_where_they_belong(K, d, kv, dtype):
+    """A query that is none makes its own row none, a key its stream's rows of its head, a value its column; no other."""
+    import torch
+    case = Case(d, kv, [300, 300, 300, 2000, 40], 16, dtype)
+    dh, group = d // case.heads, case.heads // kv
+    want = case.run()
+    case.q[1, 3] = math.nan
+    case.k[case.slots[2][17], dh * (kv - 1)] = math.nan
+    case.v[case.slots[3][1999], 5] = math.inf
+    got = case.run()
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    bad[1, :dh] = True
+    bad[2, d - dh * group:] = True
+    for g in range(group):
+        bad[3, g * dh + 5] = True
+    assert (torch.isfinite(got) == ~bad).all() and torch.equal(got[~bad], want[~bad])
+    case.enc.close()
+
+
+def test_two_contexts_on_two_streams(K):
+    """Long streams in pieces, on both at once: each has its own work space."""
+    import torch
+    cases = [Case(256, 8, [20_000, 3, 9_000], 16, "bf16", seed=1), Case(256, 2, [9_000, 15_000], 32, "bf16", seed=2)]
+    want = [c.run() for c in cases]
+    sides = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(6):
+        for side, c, o in zip(sides, cases, outs):
+            with torch.cuda.stream(side):
+                o.append(c.run())
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert all(torch.equal(x, w) for x in o)
+    for c in cases:
+        c.enc.sync_status()
+        c.enc.close()
 
 
 def test_rows_past_32_bits(K):
