@@ -10,6 +10,7 @@
 // them up in order.  Units lie on multiples of 32 positions and pages hold 8 or more, so eight consecutive tokens of
 // a unit are in one page.
 #include <algorithm>
+#include <cstddef>
 #include <type_traits>
 
 #include "kernels.h"
@@ -91,8 +92,10 @@ constexpr float kSlack = 16.f;
 template <int ROWS, int DH>
 struct Rows {
   float m[ROWS], l[ROWS];
-  float o[ROWS][DH];
+  alignas(16) float o[ROWS][DH];   // (16 bytes are written and read at once)
 };
+template <typename R>
+constexpr bool rows_are_aligned(int bytes) { return offsetof(R, o) % 16 == 0 && bytes % 16 == 0; }
 
 // bf16, several query heads a key head.  A wavefront has 128 bytes of every key and value row, a slab: NH key heads, and up to 16 query heads of each.
 // Logits are products of 16 tokens x 32 features x 16 query heads, S^T = K Q^T, which leave lane l query head l mod 16 and tokens
@@ -109,6 +112,7 @@ struct Core16 {
   static constexpr int kBytes = 2 * kUnit * 128;   // LDS of a tile: keys, values
   typedef Rows<kRows, DH> Result;
   static_assert(sizeof(Result) <= kBytes, "in place of keys and values");
+  static_assert(rows_are_aligned<Result>(kBytes), "rows pass 16 bytes at a time");
 
   static __device__ __forceinline__ void run(const MemoryAttentionArgs& a, unsigned char* lds, int b, int slab, int group, int unit, int step,
                                              int units, int first, int end) {
@@ -356,6 +360,7 @@ struct CoreLanes {
   static constexpr int kSlabHeads = kPieces < 8 ? 8 / kPieces : 1, kGroup = GROUP, kRows = kSlabHeads * GROUP;
   typedef Rows<kRows, DH> Result;
   static constexpr int kBytes = (sizeof(Result) + 255) / 256 * 256;
+  static_assert(rows_are_aligned<Result>(kBytes), "rows pass 16 bytes at a time");
 
   static __device__ __forceinline__ void run(const MemoryAttentionArgs& a, unsigned char* lds, int b, int slab, int group, int unit, int step,
                                              int units, int first, int end) {
