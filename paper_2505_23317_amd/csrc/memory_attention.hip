@@ -235,7 +235,10 @@ struct Core16 {
               s[h][half16] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][half16][c], *reinterpret_cast<const bf16x8*>(&qf[h][c]), s[h][half16], 0, 0, 0);
           }
         const uint32_t open = __builtin_amdgcn_readlane((int)t.open, i);
-        bf16x8 w[NH];
+        union {
+          uint32_t part[4];
+          bf16x8 whole;
+        } w[NH][2];
 #pragma unroll
         for (int h = 0; h < NH; ++h) {
           if (open != 0xFFFFFFFFu) {
@@ -273,16 +276,22 @@ struct Core16 {
 #pragma unroll
           for (int r = 0; r < 8; ++r) sum += p[r];
           l_run[h] += sum;
-          // a rounding of the weights: half a step of 2^-8 each, the sum takes them as they were.  (What it
-          // leaves in a second product: rows off by 0.0017 of their size instead of 0.0023, most of it the output's own rounding, for
-          // 1 to 3 % of the time of long streams and 3 to 9 % of short ones'.)
-          const uint4 packed = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-          w[h] = *reinterpret_cast<const bf16x8*>(&packed);
+          // A weight goes into two products, itself rounded to bf16 and what that leaves, rounded to bf16: off by 2^-16 of itself
+          // and not by 2^-8, rows by 0.0017 of their size and not by 0.0023 (their own rounding is 0.0017).  The second costs 24 streams
+          // of 8,000 to 64,000, 768 / 2, 47.1 -> 47.3 us, one of 1,600, 256 / 4, 10.9 -> 11.4, 300 of up to 900, 256 / 4, 15.5 -> 16.7.
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const uint32_t hi = pack_bf16x2(p[2 * r], p[2 * r + 1]);
+            w[h][0].part[r] = hi;
+            w[h][1].part[r] = pack_bf16x2(p[2 * r] - __uint_as_float(hi << 16), p[2 * r + 1] - __uint_as_float(hi & 0xFFFF0000u));
+          }
         }
 #pragma unroll
-        for (int h = 0; h < NH; ++h)
+        for (int of = 0; of < 2; ++of)
 #pragma unroll
-          for (int n = 0; n < NB; ++n) acc[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h][n].whole, w[h], acc[h][n], 0, 0, 0);
+          for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h][n].whole, w[h][of].whole, acc[h][n], 0, 0, 0);
       }
     }
     // (the LDS of keys and values is free: every read has been waited for)
@@ -769,10 +778,9 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
 }
 
 // Key heads of one query head go through lanes, those of several through matrix products, whose time is that of 16.  bf16, us:
-// one query head, 256 wide in heads of 32: one stream of 1,600 tokens 10.2 by lanes, 11.0 by products; 1,024 of up to 100 18.4 and
-// 20.3; heads of 64, width 768: 10.5 and 9.9, one stream of 200,003 115.6 and 115.8, and rows off by 0.0017 of their size instead of
-// 0.0023 (lanes keep the weights in 32 bits).  Two query heads: one stream of 1,600, 256 / 4 key heads, 12.3 and 10.8, 300 of
-// up to 900 18.5 and 15.4.
+// one query head, 256 wide in heads of 32: one stream of 1,600 tokens 10.1 by lanes, 11.9 by products; 1,024 of up to 100 18.4 and
+// 21.5; heads of 64, width 768: 10.5 and 10.3, one stream of 200,003 116 and 116, and weights stay in 32 bits.  Two query
+// heads: one stream of 1,600, 256 / 4 key heads, 12.3 and 11.4, 300 of up to 900 18.5 and 16.7.
 template <int DH>
 hipError_t launch(const MemoryAttentionArgs& a, bool use_bf16, int cus, hipStream_t s) {
   const int G = a.heads / a.kv_heads;
