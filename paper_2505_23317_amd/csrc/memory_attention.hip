@@ -88,6 +88,15 @@ __device__ __forceinline__ float across_quarters(float v, F f) {
 // multiplied less often.  A weight is 2^kSlack at most; the header promises sums for values below 2^110 / n.
 constexpr float kSlack = 16.f;
 
+// A logit in base 2, rounded: not part of a fused multiply-add, so that the largest one less itself is 0 whatever its size.
+__device__ __forceinline__ float in_base_2(float s, float scale2) {
+#pragma clang fp contract(off)
+  return s * scale2;
+}
+// A fused multiply-add less the reference has what the reference's rounding left, 2^-25 of it: nothing beside kSlack up to here,
+// past 2^31 more than a weight can hold.
+constexpr float kFar = 1048576.f;
+
 // What a wavefront leaves of its tiles: for row i of its kRows (query heads) a maximum, a sum and a row under that maximum.
 template <int ROWS, int DH>
 struct Rows {
@@ -134,6 +143,7 @@ struct Core16 {
     }
     f32x4 acc[NH][NB];
     float m_run[NH], l_run[NH], ref[NH];   // ref: m_run, or 0 as long as no token is open
+    uint64_t far = 0;                      // lanes with a reference past kFar
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       m_run[h] = -INFINITY;
@@ -253,8 +263,13 @@ struct Core16 {
           // then need not wait for the maximum.
           float p[8];
           auto weigh = [&] {
+            if (__builtin_expect(far == 0, 1)) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[h][r >> 2][r & 3], a.scale2, -ref[h]));
+              for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[h][r >> 2][r & 3], a.scale2, -ref[h]));
+            } else {
+#pragma unroll
+              for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(in_base_2(s[h][r >> 2][r & 3], a.scale2) - ref[h]);
+            }
           };
           weigh();
 #pragma unroll
@@ -262,11 +277,12 @@ struct Core16 {
           float top = s[h][0][0];
 #pragma unroll
           for (int r = 1; r < 8; ++r) top = fmaxf(top, s[h][r >> 2][r & 3]);
-          top = across_quarters(top, [](float x, float y) { return fmaxf(x, y); }) * a.scale2;
+          top = in_base_2(across_quarters(top, [](float x, float y) { return fmaxf(x, y); }), a.scale2);
           const bool follow = top > m_run[h] + kSlack;
           if (__any(follow)) {
             const float alpha = follow ? __builtin_amdgcn_exp2f(m_run[h] - top) : 1.0f;
             if (follow) m_run[h] = ref[h] = top;
+            far |= __ballot(fabsf(ref[h]) > kFar);
             l_run[h] *= alpha;
 #pragma unroll
             for (int n = 0; n < NB; ++n) acc[h][n] *= alpha;
@@ -425,7 +441,7 @@ struct CoreLanes {
 #pragma unroll
         for (int h = 0; h < GROUP; ++h)
 #pragma unroll
-          for (int j = 0; j < LOADS; ++j) s[h][j] = row_sum<kPieces>(Bytes16<T>::dot(q[h], k[j])) * a.scale2;
+          for (int j = 0; j < LOADS; ++j) s[h][j] = in_base_2(row_sum<kPieces>(Bytes16<T>::dot(q[h], k[j])), a.scale2);
         if (open != 0xFFFFFFFFu) {
 #pragma unroll
           for (int j = 0; j < LOADS; ++j)

@@ -1,4 +1,5 @@
-"""How exact the operators of a stream memory are, against the formulas in 64 bits: weights of shared key heads."""
+"""How exact the operators of a stream memory are, against the formulas in 64 bits: weights of shared key heads, logits of any
+size."""
 import pytest
 
 import differential_reference as T
@@ -33,5 +34,36 @@ def test_weights_of_shared_key_heads(K, d, kv, page):
     n = max(len(s) for s in case.slots)
     off = off + want * (2.0 ** -16 + n * T.EPS32)
     T.within(got, want, off + T.HALF_STEP["bf16"] * (want + off), "rows")
+    case.enc.sync_status()
+    case.enc.close()
+
+
+@pytest.mark.parametrize("d,kv,dtype", [(256, 8, "bf16"), (256, 4, "bf16"), (384, 2, "bf16"), (768, 1, "bf16"), (64, 2, "f32"), (384, 2, "f32"), (768, 2, "f32")])
+@pytest.mark.parametrize("exponent", (14, 20, 28))
+def test_logits_past_a_billion(K, d, kv, dtype, exponent):
+    """Logits of 2^28 to 2^56, thousands and more apart: a row is the value of the token with the largest, bit by bit, wherever that is.
+
+    Queries are 2^exponent and one feature makes the difference: the logit of a key is its first feature times 2^exponent times the
+    scale.  The largest key has 3/2 of 2^exponent there, the others -1 to 1 of it: products and sums are exact in 32 bits but for
+    the scale, and e to the differences is 0.
+    """
+    import torch
+    lengths = [1, 40, 700, 700, 9000]
+    case = Case(d, kv, lengths, 16, dtype, std=1.0)
+    dh, group = d // case.heads, case.heads // kv
+    big = 2.0 ** exponent
+    case.q.zero_()
+    case.q[:, ::dh] = big
+    top = [0, 39, 0, 350, 8000]
+    for b, (slots, t) in enumerate(zip(case.slots, top)):
+        at = torch.as_tensor(slots, device="cuda")
+        first = (torch.rand(len(slots), kv, generator=torch.Generator(device="cuda").manual_seed(b), device="cuda") * 2 - 1) * big
+        first[t] = 1.5 * big
+        for h in range(kv):
+            case.k[at, h * dh] = first[:, h].to(T.act(dtype))
+    got = case.run()
+    for b, (slots, t) in enumerate(zip(case.slots, top)):
+        want = case.v[slots[t]].view(kv, 1, dh).expand(kv, group, dh).reshape(d)
+        assert torch.equal(got[b], want), (b, exponent)
     case.enc.sync_status()
     case.enc.close()
