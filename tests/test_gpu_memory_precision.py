@@ -1,10 +1,14 @@
 """How exact the operators of a stream memory are, against the formulas in 64 bits: weights of shared key heads, logits of any
-size."""
+size, rotations in the check mode."""
+import math
+
+import numpy as np
 import pytest
 
 import differential_reference as T
 import stream_memory_reference as R
 from test_gpu_memory_attention import Case
+from test_gpu_memory_rows import _positions, _table
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +71,51 @@ def test_logits_past_a_billion(K, d, kv, dtype, exponent):
         assert torch.equal(got[b], want), (b, exponent)
     case.enc.sync_status()
     case.enc.close()
+
+
+def _in_32_bits(x, pos, axis, freq, heads, interleaved):
+    """Features turned by sines and cosines rounded to 32 bits: b s rounded, a c added to it and rounded once."""
+    import torch
+    rows, n = x.shape[0], len(axis)
+    y = x.reshape(rows, heads, -1).clone()
+    angle = pos.double()[:, torch.tensor(axis, device=x.device)] * torch.tensor(freq, dtype=torch.float64, device=x.device)
+    c, s = angle.cos().float()[:, None], angle.sin().float()[:, None]
+    i = torch.arange(n, device=x.device)
+    ia, ib = (2 * i, 2 * i + 1) if interleaved else (i, i + n)
+    a, b = y[..., ia], y[..., ib]
+    y[..., ia], y[..., ib] = (a.double() * c.double() - (b * s).double()).float(), (a.double() * s.double() + (b * c).double()).float()
+    return y.reshape(rows, -1)
+
+
+@pytest.mark.parametrize("d,kv,pairs,interleaved,far", [(64, 1, (4, 6, 6), False, 160), (384, 2, (8, 12, 12), True, 4000), (768, 12, (4, 6, 6), True, 1_000_003),
+                                                        (768, 4, (32,), False, 16_000_000)])
+def test_rotation_in_the_check_mode(K, d, kv, pairs, interleaved, far):
+    """fp32: sine and cosine are those of the angle, rounded to 32 bits; the rest is one product and one fused multiply-add.
+
+    Bound, relative to a pair's length: sine and cosine half a step each, 2^-24 of the length together (|a c| + |b s| is at most the
+    length), 2^-24 for the product and 2^-24 for the sum; second orders, a thousandth.  The angle: five roundings in 64
+    bits on either side (frequency, product, turns) of at most `far` radians.
+    Bits: those of the same two operations on the rounded sines and cosines, which 64 bits hold but for a bit that decides a tie
+    in one of 2^28: what differs is what the angle's last 64 bits move over a border of 32, 5 far 2^-53 of 2^-24 radians.
+    """
+    import torch
+    rows = 400
+    enc, heads = T.encoder(d, 8, dtype="f32"), T.MODELS[d]
+    kd = d // heads * kv
+    params = K.rotary_axes_params(2 * sum(pairs), pairs, False, False, interleaved)
+    axis, freq = R.axes_table(pairs, False, False)
+    pos = _positions(rows, len(pairs), far, 1)
+    qk = T.normal(2, rows, d + kd)
+    out = torch.empty_like(qk)
+    enc.rotary_axes(params, *_table(K, params), pos, qk[:, :d], out[:, :d], qk[:, d:], out[:, d:])
+    for x, got, n in ((qk[:, :d], out[:, :d], heads), (qk[:, d:], out[:, d:], kv)):
+        want, size = R.turned(x, pos, axis, freq, n, interleaved)
+        T.within(got, want, size * (3.003 * T.EPS32 + 5 * far * 2.0 ** -53), "features")
+        same = _in_32_bits(x, pos, axis, freq, n, interleaved)
+        assert (got != same).double().mean() < 1e-4 + 40 * far * 2.0 ** -29
+    cache = torch.empty(rows // 8 * 8, kd, device="cuda"), torch.empty(rows // 8 * 8, kd, device="cuda")
+    enc.attach_memory(8, rows // 8, 4, 1, kv)
+    slots = torch.arange(rows, dtype=torch.int32, device="cuda")
+    enc.memory_append(qk[:, d:], qk[:, d:], slots, *cache, params, *_table(K, params), pos)
+    assert torch.equal(cache[0], out[:, d:]) and torch.equal(cache[1], qk[:, d:])   # the same bits as the rotation's
+    enc.close()
