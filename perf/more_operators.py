@@ -346,23 +346,40 @@ def run(s):
     return {"advance": _plain_advance, "rotary": _plain_rotary, "append": _plain_append, "attention": _plain_attention}[s["case"]["op"]](s)
 
 
-def _own_state(case, s):
-    """The context of a program with this model and memory, and the pairs' table as the library lays it out."""
+def _context(width, heads, dtype, memory, made={}):
+    """The context of a program with this model and memory: made once, whatever inputs come (sizes and work space are all it has of them)."""
     from paper_2505_23317_amd import cfdetr, synth
 
+    key = (width, heads, dtype, memory)
+    if key not in made:
+        cfg = synth.Config("operators", 1, 32, 32, (32,), width, heads, 1, 2 * width, "bf16")
+        made[key] = cfdetr.Encoder(cfg, synth.make_weights(cfg, 1), act_dtype=dtype, max_batch=1, max_tokens_total=64)
+        if memory:
+            made[key].attach_memory(*memory)
+    return made[key]
+
+
+def _rotation(rot_dim, pairs, in_turn, shared, interleaved, made={}):
+    """Parameters of a rotation and the pairs' table as the library lays it out, which depend on no input."""
+    from paper_2505_23317_amd import cfdetr
+
+    key = (rot_dim, pairs, in_turn, shared, interleaved)
+    if key not in made:
+        params = cfdetr.rotary_axes_params(rot_dim=rot_dim, pairs=pairs, in_turn=in_turn, shared_ladder=shared, interleaved=interleaved)
+        freq, axis = cfdetr.cfdetr_rotary_axes_table(params)
+        made[key] = (params, torch.tensor(freq, dtype=torch.float64, device="cuda"), torch.tensor(axis, dtype=torch.uint8, device="cuda"))
+    return made[key]
+
+
+def _own_state(case, s):
     op = case["op"]
-    d, heads = case.get("width", 256), case.get("heads", 8)
-    cfg = synth.Config("operators", 1, 32, 32, (32,), d, heads, 1, 2 * d, "bf16")
-    s["enc"] = cfdetr.Encoder(cfg, synth.make_weights(cfg, 1), act_dtype=case.get("dtype", "bf16"), max_batch=1, max_tokens_total=64)
+    memory = None
     if op != "rotary":
-        s["enc"].attach_memory(page_size=case["page"], n_pages=s["n_pages"], max_pages=s.get("cols", 1),
-                               max_streams=case.get("streams", 1), n_kv_heads=case.get("key_heads"))
+        memory = (case["page"], s["n_pages"], s.get("cols", 1), case.get("streams", 1), case.get("key_heads"))
+    s["enc"] = _context(case.get("width", 256), case.get("heads", 8), case.get("dtype", "bf16"), memory)
     if op in ("rotary", "append"):
-        s["params"] = cfdetr.rotary_axes_params(rot_dim=_rot_dim(case), pairs=_sections(case), in_turn=case.get("in_turn", False),
-                                                shared_ladder=case.get("shared", False), interleaved=case.get("interleaved", False))
-        freq, axis = cfdetr.cfdetr_rotary_axes_table(s["params"])
-        s["freq"] = torch.tensor(freq, dtype=torch.float64, device="cuda")
-        s["axis"] = torch.tensor(axis, dtype=torch.uint8, device="cuda")
+        s["params"], s["freq"], s["axis"] = _rotation(_rot_dim(case), tuple(_sections(case)), case.get("in_turn", False),
+                                                      case.get("shared", False), case.get("interleaved", False))
 
 
 def _own_run(s):
