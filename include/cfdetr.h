@@ -165,7 +165,7 @@ CFDETR_API void cfdetr_destroy(cfdetr_ctx* ctx);
  * ctx == NULL: the reason the calling thread's last cfdetr_create failed.  The
  * pointer stays valid until the next failing call. */
 CFDETR_API const char* cfdetr_last_error(const cfdetr_ctx* ctx);
-/* Bytes of device work space the context holds. */
+/* Bytes of device work space the context holds, that of what is attached to it included. */
 CFDETR_API uint64_t cfdetr_workspace_bytes(const cfdetr_ctx* ctx);
 /* Waits for `hip_stream`, then reports and clears the device-side sticky flag:
  * CFDETR_OK, or CFDETR_ECAPACITY if a selection overflowed max_tokens_total. */

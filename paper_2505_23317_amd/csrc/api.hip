@@ -29,7 +29,7 @@ struct cfdetr_ctx {
 
   // one device allocation, carved up
   void* arena = nullptr;
-  uint64_t arena_bytes = 0;
+  uint64_t arena_bytes = 0;   // with those of the decoder, the differential layers and the memory
   float* x = nullptr;      // residual stream [Tm, d] fp32
   void* a = nullptr;       // LayerNorm output [Tm, d]
   void* qkv = nullptr;     // [Tm, 3d]
@@ -1807,6 +1807,7 @@ CFDETR_API cfdetr_status cfdetr_decoder_attach(cfdetr_ctx* ctx, const cfdetr_dec
   ctx->dw = *w;
   ctx->dtail_packed_layer = tail_bytes;
   ctx->dwide_layer = wide_bytes;
+  ctx->arena_bytes += cv.off;
   ctx->has_dec = true;
   return CFDETR_OK;
 }
@@ -2014,6 +2015,7 @@ CFDETR_API cfdetr_status cfdetr_differential_attach(cfdetr_ctx* ctx, const cfdet
   ctx->diff_freq = reinterpret_cast<double*>(base + o_freq);
   ctx->diff_pos = reinterpret_cast<float*>(base + o_pos);
   ctx->fw = *w;
+  ctx->arena_bytes += cv.off;
   ctx->has_diff = true;
   return CFDETR_OK;
 }
@@ -2050,6 +2052,7 @@ CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memo
   ctx->mem = *cfg;
   ctx->mem_page_bits = 0;
   while ((1 << ctx->mem_page_bits) < cfg->page_size) ++ctx->mem_page_bits;
+  ctx->arena_bytes += cv.off;
   ctx->has_mem = true;
   return CFDETR_OK;
 }
