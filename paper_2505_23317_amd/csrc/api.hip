@@ -258,7 +258,7 @@ void rotary_frequencies(const cfdetr_rotary_params& p, double* freq) {
 constexpr int kMaxRowElements = 1 << 24;
 const char* check_rows(const cfdetr_ctx* ctx, const void* p, int ld, int columns) {
   if (!p) return "null pointer";
-  if (ld < columns || ld > kMaxRowElements) return "rows must be d_model to 2^24 elements apart";
+  if (ld < columns || ld > kMaxRowElements) return "rows must be as far apart as they have columns, and 2^24 elements at most";
   if (!aligned16(p) || (size_t)ld * ctx->esz % 16) return "rows must begin on multiples of 16 bytes";
   return nullptr;
 }

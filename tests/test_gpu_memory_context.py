@@ -1,4 +1,4 @@
-"""What a context says of a memory of streams: its work space."""
+"""What a context says of a memory of streams: its work space, and why it refuses rows."""
 import pytest
 
 import differential_reference as T
@@ -40,4 +40,21 @@ def test_work_space_counts_the_differential_layers(K):
     bare = K.cfdetr_workspace_bytes(enc.ctx)
     enc.attach_differential({"lambda": torch.zeros(1, 1).numpy()}, K.rotary_params(32))
     assert K.cfdetr_workspace_bytes(enc.ctx) - bare >= 100 * 8
+    enc.close()
+
+
+def test_rows_of_keys_are_refused_for_their_own_width(K):
+    """The reason names no width that the rows need not have: a key row here is 32 wide, a query row 64."""
+    import torch
+    enc = T.encoder(64, 8)
+    enc.attach_memory(8, 4, 4, 2, 1)
+    x = torch.zeros(64, 64, device="cuda", dtype=torch.bfloat16)
+    i = torch.zeros(64, dtype=torch.int32, device="cuda")
+    p, n = x.data_ptr(), i.data_ptr()
+    for call in (lambda: K.cfdetr_memory_attention(enc.ctx, p, 64, 2, p, 24, p, 32, n, n, None, 0.1, p, 64, enc._stream()),
+                 lambda: K.cfdetr_memory_append(enc.ctx, None, None, None, None, 1, p, 24, p, 32, n, p, 32, p, 32, enc._stream())):
+        with pytest.raises(K.CfdetrError) as e:
+            call()
+        assert e.value.status == K.CFDETR_EINVAL and "apart" in K.cfdetr_last_error(enc.ctx) and "d_model" not in K.cfdetr_last_error(enc.ctx)
+    enc.sync_status()
     enc.close()
