@@ -6,8 +6,6 @@
 // sums over the streams of the numbers taken and given back.  Every workgroup works them out for itself from all streams'
 // spans, then takes its share of the slots and page numbers, so that a step is one launch.  A few microseconds
 // of latency bound it: one round of loads for the spans, the sums, one for the page numbers.
-#include <algorithm>
-
 #include "kernels.h"
 #include "stream_memory.h"
 
@@ -15,7 +13,7 @@ namespace cfdetr {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kThreads = kAdvanceThreads, kWaves = kThreads / 64;
 
 struct Sums {
   int taken, given, work;
@@ -200,12 +198,8 @@ hipError_t launch(const MemoryAdvanceArgs& a, int grid, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_memory_advance(const MemoryAdvanceArgs& a, int cus, hipStream_t s) {
-  // a workgroup a CU at most; a single workgroup needs no counting at the end
-  const bool many = a.n_new > kThreads * cus;
-  const int64_t slots = ((int64_t)a.n_new + (many ? 4 : 1) * kThreads - 1) / ((many ? 4 : 1) * kThreads);
-  const int64_t pages = a.table_out != a.table ? ((int64_t)a.B * a.cols + 8 * kThreads - 1) / (8 * kThreads) : 0;
-  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(cus, std::max(slots, pages)));
-  return many ? launch<4>(a, grid, s) : launch<1>(a, grid, s);
+  const AdvanceLaunch l = advance_launch(a.n_new, a.B, a.cols, a.n_pages, a.drop != nullptr, a.table_out != a.table, cus);
+  return l.chunk == 4 ? launch<4>(a, l.grid, s) : launch<1>(a, l.grid, s);
 }
 
 }  // namespace cfdetr

@@ -95,6 +95,26 @@ constexpr int stream_of(const Offsets& offsets, int n, int at) {
   return lo;
 }
 
+// Workgroups of a step, one a CU at most, and consecutive slots of a thread.  What the step has to do is known on the device only: a
+// slot for every new token, and of page numbers those that may go or move, all entries of a table that lies apart, and of
+// one in place, if tokens are forgotten, as many as there are pages at most.  Two rounds of numbers a workgroup, us: 300 streams of 700 tokens, page 16, in
+// place, all lost 10.7 (one workgroup 46, eight rounds 18, one 9.4), a quarter of 1,024 of 3,000, page 32, 11.1 (46, 12.2, 12.0), one of 200,000,
+// page 8, 8.9 (40.5, 12.2, 8.3); where they only slide by a token several workgroups take longer, 300 streams 8.1 (one 7.1).  Apart, 300 streams
+// that slide 9.9 (eight rounds 14.5, one 8.5).
+constexpr int kAdvanceThreads = 512;
+struct AdvanceLaunch {
+  int chunk, grid;
+};
+constexpr AdvanceLaunch advance_launch(int n_new, int streams, int cols, int n_pages, bool forgets, bool apart, int cus) {
+  constexpr int64_t T = kAdvanceThreads;
+  const int64_t entries = (int64_t)streams * cols;
+  const int64_t numbers = apart ? entries : !forgets ? 0 : entries < n_pages ? entries : n_pages;
+  const int chunk = n_new > T * cus ? 4 : 1;
+  const int64_t slots = (n_new + chunk * T - 1) / (chunk * T), pages = (numbers + 2 * T - 1) / (2 * T);
+  const int64_t most = slots > pages ? slots : pages;
+  return {chunk, (int)(most < 1 ? 1 : most < cus ? most : cus)};
+}
+
 // Why a memory's sizes are refused; null: they are not.
 constexpr const char* check_memory_sizes(int page_size, int n_pages, int max_pages, int max_streams, int kv_heads, int heads) {
   if (page_size < 8 || page_size > 1024 || (page_size & (page_size - 1)) != 0) return "page_size must be a power of two from 8 to 1024";
