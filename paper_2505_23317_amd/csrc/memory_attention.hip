@@ -20,7 +20,7 @@ namespace cfdetr {
 
 namespace {
 
-constexpr int kUnit = 32;   // tokens
+constexpr int kUnit = kMemoryUnit;
 // Measured as replays of a captured call, us; "768 / 4": width 768, four key heads.
 // A piece has four units a wavefront at least, a stream of up to ten is not cut: adding the pieces takes 2 us and more, a tile
 // 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 10.5 (six units at least 12.1, eight 13.6; six streams of 4,000 to 16,000, 768 / 4,
@@ -567,7 +567,6 @@ struct Piece {
   int first, held;              // the stream's span
   bool bad;                     // a span is none, or there are too many units
 };
-__device__ __forceinline__ int units_of(int2 span) { return span.y > 0 ? (span.x + span.y - 1) / kUnit - span.x / kUnit + 1 : 0; }
 // The wavefronts share the streams, rows of 64 that lie behind each other.  Up to 64 streams every wavefront has them all and needs no
 // barrier (one stream of 64 tokens 6.3 us, 7.2 with all three).
 template <int NW>
@@ -591,7 +590,7 @@ __device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int pi
   for (int r = 0; r < R; ++r) {
     if (r >= rows) break;
     if (span_is_bad(span[r].x, span[r].y, a.page_bits, a.cols)) p.bad = true;
-    else units += units_of(span[r]);
+    else units += units_of(span[r].x, span[r].y);
   }
   // (the units' thousands tell whether their sum fits 32 bits)
   int total = __builtin_amdgcn_readlane(sum_upto(units), 63), thousands = __builtin_amdgcn_readlane(sum_upto((units + 1023) / 1024), 63);
@@ -614,22 +613,14 @@ __device__ __forceinline__ Piece find_piece(const MemoryAttentionArgs& a, int pi
   }
   p.bad = thousands > kMostUnits / 1024;
   if (p.bad) return p;
-  // Every stream's last piece is shorter: at most as many pieces as the length would make of one stream, and one more a stream.
-  // Few streams: no more pieces than places.
-  const int room = 2 * B <= a.places ? a.places - B : a.places;
-  const int length = max(least, (total + room - 1) / room);
+  const int length = cut_length(total, B, a.places, least);
   p.length = length;
   const float per_length = 1.0f / (float)length;
   int pieces[R], upto[R], before = 0;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r >= rows) break;
-    // ceil(units / length): units are below 2^24, the product may be one off
-    const int n = units_of(span[r]);
-    int q = (int)((float)n * per_length);
-    q += q * length < n ? 1 : 0;
-    q += q * length < n ? 1 : 0;
-    pieces[r] = n <= kUncut * (least / kLeast) ? min(n, 1) : q - ((q - 1) * length >= n ? 1 : 0);
+    pieces[r] = pieces_of(units_of(span[r].x, span[r].y), length, per_length, kUncut * (least / kLeast));
     upto[r] = before + sum_upto(pieces[r]);
     before = __builtin_amdgcn_readlane(upto[r], 63);
   }
@@ -692,7 +683,7 @@ __global__ __launch_bounds__(64 * NW, Core::kWavesSimd) void memory_attention_ke
   if ((int)blockIdx.x < a.B && a.span[blockIdx.x].y == 0)
     for (int i = tid; i < a.heads * Q; i += kThreads) store4(static_cast<T*>(a.out) + (size_t)blockIdx.x * a.out_ld + 4 * i, make_float4(0.f, 0.f, 0.f, 0.f));
   if (p.stream < 0) return;
-  const int b = p.stream, units = units_of(make_int2(p.first, p.held));
+  const int b = p.stream, units = units_of(p.first, p.held);
   const int u0 = p.number * p.length, u1 = p.pieces == 1 ? units : min(u0 + p.length, units);
   const int my_slab = slab_group * WS + wave % WS;
   Core::run(a, smem + wave * Core::kBytes, b, my_slab / passes, my_slab % passes, u0 + wave / WS, TS, u1, p.first, p.first + p.held);
@@ -789,7 +780,7 @@ hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   // One workgroup a CU has enough asked for to keep memory busy; the CU's second place is for what streams leave over.  24 streams of
   // 8,000 to 64,000, a fifth masked: 47.6 us, 51.0 with pieces for both places; one of 200,003, width 768, 115.9 and 119.4.
   a.places = std::max(1, cus / slab_groups);
-  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3((a.places + a.B) * slab_groups), dim3(64 * NW), 0, s, a);
+  hipLaunchKernelGGL((memory_attention_kernel<Core, DH, NW>), dim3(most_pieces(a.B, a.places) * slab_groups), dim3(64 * NW), 0, s, a);
   return hipGetLastError();
 }
 
@@ -811,8 +802,8 @@ hipError_t launch(const MemoryAttentionArgs& a, bool use_bf16, int cus, hipStrea
 }  // namespace
 
 MemoryAttentionSpace memory_attention_space(int max_streams, int heads, int d_head, int cus) {
-  // (as many pieces as places and streams, and slabs as query heads, at most)
-  const uint64_t pieces = (uint64_t)(cus + max_streams) * heads;
+  // (places are CUs at most, and slabs as query heads)
+  const uint64_t pieces = (uint64_t)most_pieces(max_streams, cus) * heads;
   return {pieces * sizeof(float2), pieces * d_head * sizeof(float), (uint64_t)max_streams * heads * sizeof(int32_t)};
 }
 

@@ -95,6 +95,30 @@ constexpr int stream_of(const Offsets& offsets, int n, int at) {
   return lo;
 }
 
+// ---- attention: streams cut into pieces ---------------------------------------------
+// A stream's tokens are units of 32 positions that lie on multiples of 32: at most 2^24 and one.
+constexpr int kMemoryUnit = 32;
+constexpr int units_of(int first, int held) { return held > 0 ? (first + held - 1) / kMemoryUnit - first / kMemoryUnit + 1 : 0; }
+
+// Units of all pieces but a stream's last, which is shorter: at most as many pieces as the length would make of one stream,
+// and one more a stream.  Few streams: no more pieces than places.  The launch and the pieces' room count on `most_pieces`.
+constexpr int cut_length(int units, int streams, int places, int least) {
+  const int room = 2 * streams <= places ? places - streams : places;
+  const int even = (units + room - 1) / room;
+  return even > least ? even : least;
+}
+constexpr int most_pieces(int streams, int places) { return places + streams; }
+
+// Pieces of a stream of n units: one up to `whole`, then ceil(n / length) by a product with 1 / length that may be one off.
+constexpr int pieces_of(int n, int length, float per_length, int whole) {
+  if (n <= whole) return n > 0 ? 1 : 0;
+  int q = (int)((float)n * per_length);
+  q += q * length < n ? 1 : 0;
+  q += q * length < n ? 1 : 0;
+  return q - ((q - 1) * length >= n ? 1 : 0);
+}
+
+// ---- steps: workgroups --------------------------------------------------------------
 // Workgroups of a step, one a CU at most, and consecutive slots of a thread.  What the step has to do is known on the device only: a
 // slot for every new token, and of page numbers those that may go or move, all entries of a table that lies apart, and of
 // one in place, if tokens are forgotten, as many as there are pages at most.  Two rounds of numbers a workgroup, us: 300 streams of 700 tokens, page 16, in
