@@ -623,6 +623,9 @@ CFDETR_API cfdetr_status cfdetr_memory_attach(cfdetr_ctx* ctx, const cfdetr_memo
  * If the free pages do not suffice, a stream would touch more than max_pages pages, or an argument is none (a negative drop,
  * offsets that descend or end beyond n_new, a span or pool that no step leaves), then nothing is forgotten or added for any stream: the outputs
  * are the state as it was, every slot is -1, and cfdetr_sync_status reports CFDETR_ECAPACITY.
+ * Page numbers are not among these checks: where a new token's page, in the table or the list of free ones, is none of 0 .. n_pages - 1
+ * (no step leaves such), the step is made, that token's slot is -1, and cfdetr_sync_status reports it; numbers that are given back
+ * are not looked at.
  */
 CFDETR_API cfdetr_status cfdetr_memory_advance(cfdetr_ctx* ctx, int32_t B, const int32_t* drop, const int32_t* cu_new,
                                     int32_t n_new, const int32_t* span, int32_t* span_out,
@@ -685,14 +688,15 @@ CFDETR_API cfdetr_status cfdetr_memory_append(cfdetr_ctx* ctx, const cfdetr_rota
  * Attention of one new token of every stream over all that the stream holds (its own key and value among it, once they are appended):
  * with G = n_heads / n_kv_heads, head h of out is softmax(softmax_scale q_h k_g^T) v_g over the held tokens, g = h / G.
  *   q       [B, ld] act: n_heads heads
- *   span, table  as a step leaves them.  A span that no step leaves, or 2^35 tokens and more in all, makes the call write nothing; a page number outside 0 .. n_pages - 1
+ *   span, table  as a step leaves them.  A span that no step leaves, or some 2^35 tokens in all (units of 32, counted by thousands), makes the call write nothing; a page number outside 0 .. n_pages - 1
  *           is not read (its tokens count as masked).  Both are reported by cfdetr_sync_status as CFDETR_ECAPACITY.
  *   key_mask  [n_pages * page_size] uint8 device (8-byte aligned), by slot, 0: the token is not read, whatever it holds; NULL: all are read
  *   softmax_scale  > 0; or 0: the queries have been multiplied by log2(e) / sqrt(d_head) already
  *   out     [B, ld] act; may be q (with the same ld).  The row of a stream that holds no token that may be read is 0.
  * Sums are 32-bit, of weights of up to 2^16 (the elements of v are taken to be below 2^110 / n in size for n tokens).  A v that
- * is not finite leaves NaN in its column.  Sums over many tokens may be split over the chip; they are added in a
- * fixed order, so the same call gives the same bits.
+ * is not finite leaves what is not finite in its column, an infinity or NaN.  Sums over many tokens may be split over the chip; they are added in a
+ * fixed order, so the same call gives the same bits; where they are split depends on all streams of the call, so a
+ * stream's row may differ in its last bits from that of a call with other streams beside it.
  */
 CFDETR_API cfdetr_status cfdetr_memory_attention(cfdetr_ctx* ctx, const void* q, int32_t q_ld, int32_t B, const void* k_cache,
                                       int32_t k_cache_ld, const void* v_cache, int32_t v_cache_ld,

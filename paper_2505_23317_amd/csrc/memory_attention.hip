@@ -1,8 +1,9 @@
 // Attention of one new token of every stream over the tokens that its stream holds in a paged memory:
 //   out[h] = sum_t softmax_t(scale q[h] . k[t, h / G]) v[t, h / G],   G = heads / key heads.
 //
-// One pass over keys and values, with a running maximum and sum.  Every key and value is read once for the G query
-// heads that share it: 2 G operations a byte in bf16, so memory bounds it.
+// One pass over keys and values, with a running maximum and sum.  A key and a value are read once for up to 16 query heads that
+// share them in bf16 and for up to four in fp32 (the check mode), once more for every further 16 or four: 2 G operations a byte in
+// bf16, so memory bounds it.
 //
 // A stream's tokens are units of 32 positions, cut into pieces of one length for all streams, a workgroup each (lengths are
 // known on the device only, so every workgroup works the cut out for itself).  A piece gives a row under its own maximum; a
@@ -775,6 +776,10 @@ template <typename Core, int DH, int NW>
 hipError_t launch(MemoryAttentionArgs a, int cus, hipStream_t s) {
   const int G = a.heads / a.kv_heads, passes = (G + Core::kGroup - 1) / Core::kGroup;
   const int slabs = (a.kv_heads + Core::kSlabHeads - 1) / Core::kSlabHeads * passes;
+  // Four slabs a workgroup, where their number can be cut so: it reads 512 bytes of a row together, and the streams' cut is made by a
+  // quarter of the workgroups.  24 streams of 8,000 to 30,000, 768 / 12: 210 us, two 278, one 270; 1,024 of up to 100 46, 77, 143; 300 of up
+  // to 900 53, 55, 70; only 64 of 2,000 94, 78, 74.  Eight, 1024 / 16 and / 8: 1,024 of up to 100 60 -> 40, 24 long ones 291 -> 269, but one of 50,001
+  // 39.7 -> 42.2 and 26.6 -> 35.1, 64 of 2,000 97 -> 109, 300 of up to 900 77 -> 80.
   a.wave_slabs = slabs % 4 == 0 ? 4 : slabs % 2 == 0 ? 2 : 1;
   const int slab_groups = slabs / a.wave_slabs;
   // One workgroup a CU has enough asked for to keep memory busy; the CU's second place is for what streams leave over.  24 streams of

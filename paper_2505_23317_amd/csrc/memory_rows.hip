@@ -8,7 +8,7 @@
 // whole turns in 64 bits: a far position is thousands of turns) while its features are on their way, and turns them.
 // What is left of a turn goes through the 32-bit functions in bf16 (as in rotary.hip, the same bits; off by some 2^-23 where the
 // result is rounded to 2^-8) and through the 64-bit ones in fp32, the check mode: sine and cosine are then rounded once, features
-// off by what their own operations lose.  16,063 rows of 2 x 768 columns: 30.2 -> 30.5 us for it, 187,500 of 32 10.8 -> 11.6.
+// off by what their own operations lose.  16,063 rows of 2 x 768 columns: 30.2 -> 30.5 us for it, 93,750 of 32 into a memory 10.8 -> 11.6.
 #include <algorithm>
 #include <type_traits>
 
