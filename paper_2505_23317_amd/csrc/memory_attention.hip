@@ -24,11 +24,11 @@ namespace {
 constexpr int kUnit = kMemoryUnit;
 // Measured as replays of a captured call, us; "768 / 4": width 768, four key heads.
 // A piece has four units a wavefront at least, a stream of up to ten is not cut: adding the pieces takes 2 us and more, a tile
-// 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 10.5 (six units at least 12.1, eight 13.6; six streams of 4,000 to 16,000, 768 / 4,
-// then 16.8 and 15.9 instead of 17.5); of 300: 9.1 (cut in two 10.2); 300 of up to 900, 256 wide, 21.4 (uncut up to sixteen 22.9, none 23.4).
+// 0.4 to 0.6.  One stream of 1,600 tokens, width 768: 10.5 (six units at least 12.2, eight 13.6; six streams of 4,000 to 16,000, 768 / 4,
+// then 16.7 and 16.0 instead of 17.5); of 300: 9.1 (cut in two 10.2); 300 of up to 900, 256 wide, 22.0 (uncut up to sixteen 23.1, none 23.5).
 constexpr int kLeast = 4, kUncut = 10;
-// Eight wavefronts a workgroup, two workgroups a CU: 24 streams of 8,000 to 64,000, 768 / 2, 47.6, 300 of up to 900, 256 wide, 21.4, 1,024 of
-// up to 100 18.4, one of 1,600, width 768, 10.5.  Sixteen and one: 48.4, 24.4, 31.3, 13.6; four and four: 50.7, 23.5, 19.1, 9.8.
+// Eight wavefronts a workgroup, two workgroups a CU: 24 streams of 8,000 to 64,000, 768 / 2, 47.7, 300 of up to 900, 256 wide, 22.0, 1,024 of
+// up to 100 18.3, one of 1,600, width 768, 10.5.  Sixteen and one: 49.2, 24.3, 31.3, 13.6; four and four: 51.0, 23.6, 19.2, 9.8.
 constexpr int kWaves = 8;
 constexpr int kResident = 2;   // workgroups that a CU has room for
 constexpr int kMostUnits = 1 << 30;   // of all streams
@@ -112,7 +112,7 @@ constexpr bool rows_are_aligned(int bytes) { return offsetof(R, o) % 16 == 0 && 
 // 4 (l / 16) + r of either half of the tile; these are at once the operand of O^T = V^T P^T if the products' index runs over
 // the tokens in that order, so weights never leave their lane.  Two query heads of 16 leave the products 14 parts zeros, and still they cost a
 // fraction of the loads' time.  Keys and values go straight into LDS, every wavefront's own, a tile ahead: no barrier in
-// the loop.  (Two tiles ahead leave a CU one workgroup: 24 streams of 8,000 to 64,000, 768 / 2, 50.0 instead of 47.6 us, 1,024 of up
+// the loop.  (Two tiles ahead leave a CU one workgroup, measured with one product of the weights: 24 streams of 8,000 to 64,000, 768 / 2, 50.0 instead of 47.6 us, 1,024 of up
 // to 100, 768 / 4, 30.3 instead of 19.1.)
 template <int DH>
 struct Core16 {
