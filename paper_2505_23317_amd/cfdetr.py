@@ -792,7 +792,7 @@ class Encoder:
     def attach_memory(self, page_size: int, n_pages: int, max_pages: int, max_streams: int,
                       n_kv_heads: Optional[int] = None):
         """n_kv_heads: key heads, a divisor of the context's heads; None for as many."""
-        mem = CfdetrMemoryConfig(page_size, n_pages, max_pages, max_streams, n_kv_heads or self.cfg.heads)
+        mem = CfdetrMemoryConfig(page_size, n_pages, max_pages, max_streams, self.cfg.heads if n_kv_heads is None else n_kv_heads)
         cfdetr_memory_attach(self.ctx, mem)
         self.mem, self.kv_dim, self.n_slots = mem, mem.n_kv_heads * self.cfg.d_head, n_pages * page_size
 
